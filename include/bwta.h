@@ -52,10 +52,11 @@ enum {
     BWTA_ERR_UNSUPPORTED = -4, /* unknown dtype, scale mode or path                        */
     BWTA_ERR_WORKSPACE = -5,   /* workspace NULL or smaller than bwta_workspace_bytes()    */
     BWTA_ERR_HIP = -6,         /* the HIP runtime reported an error at launch              */
-    BWTA_ERR_TOO_LARGE = -7    /* bwta_linear_static: the shape needs more than the static scratch */
+    BWTA_ERR_TOO_LARGE = -7    /* bwta_linear_static: the shape needs more than the static scratch;
+                                  operators on heads: more workgroups than one launch can have   */
 };
 
-enum { BWTA_DTYPE_FP16 = 0, BWTA_DTYPE_INT8 = 1 };
+enum { BWTA_DTYPE_FP16 = 0, BWTA_DTYPE_INT8 = 1, BWTA_DTYPE_BF16 = 2 /* the operators on heads only */ };
 enum { BWTA_SCALE_NONE = 0, BWTA_SCALE_SCALAR = 1, BWTA_SCALE_VECTOR = 2 };
 /* Which contraction kernel bwta_gemm / bwta_linear use.  AUTO picks per shape regime from
  * measurements on MI355X; the others force the wave64 popcount kernels, the int8 matrix-core
@@ -289,6 +290,113 @@ int bwta_act_scale(const void *A, int64_t lda, int M, int K, void *s, bwta_strea
  */
 int bwta_prepare_act_autoscale(const void *A, int64_t lda, int M, int K, void *s_a, void *prepared,
                                size_t prepared_bytes, int *prepared_format, bwta_stream_t stream);
+
+/*
+ * ---- Operators on heads: what a decoder block needs between its q/k/v projections and its output
+ * projection.  Queries, keys and values are 16-bit (dtype BWTA_DTYPE_FP16 or BWTA_DTYPE_BF16), one row
+ * per token, a row's heads side by side, `dim` elements each, tokens `ld` elements apart: the rows
+ * bwta_linear writes, or a part of them (heads of a fused q/k/v projection).  Rows start at 16-byte
+ * aligned addresses and ld is a multiple of 8 (BWTA_ERR_ALIGN).  Computation is in fp32, each result is
+ * rounded once to dtype.
+ */
+
+/*
+ * Norm of every query and key head and rotation by position, in one pass:
+ *   y = x * rsqrt(mean(x^2) + eps) * w      per head, with norm != 0; w [dim] in dtype, NULL is 1
+ *   (y_a, y_b) -> (y_a cos t - y_b sin t, y_a sin t + y_b cos t)    t = positions[m] * inv_freq[i]
+ * for the pairs i < rot_dim / 2: a = i, b = i + rot_dim / 2, or with interleaved != 0 a = 2 i,
+ * b = 2 i + 1.  Elements from rot_dim on are not rotated.  Angles are formed in fp64.
+ *   Q [M, heads, dim], K [M, kv_heads, dim]   either may have 0 heads (and be NULL)
+ *   dim        a multiple of 16, at most 256; rot_dim a multiple of 16, 0 to dim
+ *   eps        finite, >= 0 (BWTA_ERR_UNSUPPORTED)
+ *   positions  int32 [M], any values; inv_freq fp32 [rot_dim / 2].  Both may be NULL if rot_dim is 0.
+ *   Qout, Kout may be the rows they are made from (same address and ld); any other overlap of a result
+ *              with an operand or with the other result is refused (BWTA_ERR_UNSUPPORTED).
+ */
+int bwta_head_norm_rope(const void *Q, int64_t ldq, int heads, const void *wq, const void *K, int64_t ldk, int kv_heads,
+                        const void *wk, int dtype, int M, int dim, int norm, float eps, const int32_t *positions,
+                        const float *inv_freq, int rot_dim, int interleaved, void *Qout, int64_t ldqo, void *Kout,
+                        int64_t ldko, bwta_stream_t stream);
+
+/*
+ * A cache of keys and values in 8 bits.  It consists of blocks of `block` tokens; a sequence has its
+ * tokens in the blocks that its row of a block table names, in order.  Codes are E4M3 (bias 7, largest
+ * 448); each block has one scale per head for its keys and one for its values, a power of two 2^e:
+ *   x ~ code * 2^e,   e the smallest with max |x| <= 448 * 2^e over the block's finite values,
+ *   -40 <= e <= 40 (a block of zeros has -40)
+ * so the code is x / 2^e rounded once, to nearest even.
+ *   k        [blocks, kv_heads, block, dim] codes         16-byte aligned
+ *   v        [blocks, kv_heads, dim, block] codes         16-byte aligned: a channel's tokens in a row
+ *   k_scale, v_scale   fp32 [blocks, kv_heads]
+ *   block    64, 128 or 256; dim 64, 128 or 256 (BWTA_ERR_UNSUPPORTED)
+ * The struct is the caller's, on the host, and read during the call only.  Memory of blocks that hold
+ * no token yet need not be initialised.
+ */
+typedef struct bwta_cache {
+    void *k, *v;
+    float *k_scale, *v_scale;
+    int32_t blocks, kv_heads, block, dim;
+} bwta_cache;
+
+/*
+ * Sequences, in the three calls below.  The rows of the dense arrays belong to `batch` sequences, one
+ * after the other: sequence b has rows cu[b] to cu[b + 1] - 1 (cu int32 [batch + 1]), or with cu NULL
+ * max_new rows each (batch * max_new <= M).  They are its LAST tokens: lens[b] (int32 [batch]) counts
+ * the sequence's tokens with them, so row cu[b] + i is token lens[b] - n_b + i, n_b = cu[b + 1] - cu[b].
+ *   M        rows of the dense arrays; rows of no sequence are neither read nor written
+ *   max_new  at least every n_b: rows behind it are left out;  max_len  at least every lens[b]:
+ *            larger ones count as max_len.  Both are the host's bounds for the launch; a captured
+ *            graph may be replayed with other lens, cu and table contents inside them.
+ *   table    int32, sequence b's row at table + b * ldt, ldt >= ceil(max_len / block); an entry outside
+ *            [0, blocks) is a block that is not there (see the calls).
+ * lens, cu and table are device memory, 4-byte aligned.
+ */
+
+/*
+ * Writes the rows' keys K and values V [M, kv_heads, dim] into their blocks.  A block whose first token
+ * is among the rows starts anew; in any other the scale can only grow: if the new tokens need a larger e, all
+ * codes of the block are divided by the ratio and rounded again (exact but for values that become
+ * subnormal).  NaN is written as 0, +-Inf as +-448 * 2^e.  Slots behind a sequence's last token get
+ * no token's code.  Tokens of blocks that are not there, and rows of negative position, are not written.
+ * Blocks that are written must each be named once among all sequences' written parts; sequences may
+ * share the blocks before that.
+ */
+int bwta_cache_write(const bwta_cache *cache, const void *K, int64_t ldk, const void *V, int64_t ldv, int dtype,
+                     const int32_t *table, int64_t ldt, const int32_t *lens, const int32_t *cu, int batch, int M,
+                     int max_new, int max_len, bwta_stream_t stream);
+
+/*
+ * The rows' keys and values back as 16-bit numbers: code * 2^e rounded to dtype, beyond its range its
+ * largest.  Tokens of blocks that are not there give 0; rows of negative position are left as they are.
+ * For whole sequences let cu be the sums of lens.
+ */
+int bwta_cache_read(const bwta_cache *cache, void *K, int64_t ldk, void *V, int64_t ldv, int dtype, const int32_t *table,
+                    int64_t ldt, const int32_t *lens, const int32_t *cu, int batch, int M, int max_new, int max_len,
+                    bwta_stream_t stream);
+
+/*
+ * Attention of the rows' queries over their sequences' cached tokens:
+ *   out[m, h] = sum_j p_j v_j,  p = softmax over the tokens j that the row sees of alpha * q[m, h] . k_j
+ *   lse[m, h] = log sum_j exp(alpha * q[m, h] . k_j)       natural logarithm
+ * Query head h reads key head h / (heads / kv_heads).  A row of position p sees with causal != 0 the
+ * tokens up to p (itself among them: write first, then attend), with window > 0 of these the last
+ * `window`; with causal == 0 all lens[b] tokens (an encoder's states: then the rows need not be in the
+ * cache).  Tokens of blocks that are not there are not seen.  A row that sees nothing gets 0, and -Inf
+ * in lse.
+ *   heads    a multiple of the cache's kv_heads
+ *   alpha    finite and > 0; window >= 0, and 0 unless causal (BWTA_ERR_UNSUPPORTED)
+ *   out      [M, heads, dim] in dtype; may be Q itself (same address and ld), must not overlap it else
+ *   lse      optional, fp32 [M, heads] dense
+ *   workspace  bwta_cache_attention_workspace_bytes of the same numbers, 256-byte aligned, contents
+ *            undefined before and after; may be NULL if that is 0.  Calls that share one must not overlap.
+ * A code of NaN, which bwta_cache_write never writes, makes NaN of every row that sees its key, and of any
+ * row of the sequence if it is a value's.
+ */
+size_t bwta_cache_attention_workspace_bytes(int M, int heads, int kv_heads, int dim, int batch, int max_new, int max_len);
+int bwta_cache_attention(const bwta_cache *cache, const void *Q, int64_t ldq, void *out, int64_t ldo, int dtype, float *lse,
+                         const int32_t *table, int64_t ldt, const int32_t *lens, const int32_t *cu, int batch, int M,
+                         int max_new, int max_len, int heads, float alpha, int causal, int window, void *workspace,
+                         size_t workspace_bytes, bwta_stream_t stream);
 
 /* Human-readable text for a return code (static storage). */
 const char *bwta_strerror(int code);

@@ -27,7 +27,7 @@ NATIVE_PATH = os.path.join(_HERE, "csrc", "_bwta_native.so")
 
 OK = 0
 ERR_NULL, ERR_SHAPE, ERR_ALIGN, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_HIP, ERR_TOO_LARGE = -1, -2, -3, -4, -5, -6, -7
-DTYPE_FP16, DTYPE_INT8 = 0, 1
+DTYPE_FP16, DTYPE_INT8, DTYPE_BF16 = 0, 1, 2
 SCALE_NONE, SCALE_SCALAR, SCALE_VECTOR = 0, 1, 2
 PATH_AUTO, PATH_POPC, PATH_MFMA, PATH_FP4 = 0, 1, 2, 3
 PREPARED_PLANES, PREPARED_FP4 = 1, 2
@@ -42,7 +42,8 @@ EXPORTS = ["bwta_plane_row_words", "bwta_workspace_bytes", "bwta_quantize_pack_a
            "bwta_set_tile", "bwta_planned_tile", "bwta_planned_wide", "bwta_planned_wide_prepared", "bwta_planned_rows", "bwta_planned_decode_blocks",
            "bwta_prepared_bytes", "bwta_prepared_format", "bwta_planned_kernel", "bwta_prepare_act", "bwta_gemm_prepared", "bwta_gemm_grouped",
            "bwta_quantize_pack_bool", "bwta_matmul_tt", "bwta_prepare_weights", "bwta_act_scale",
-           "bwta_prepare_act_autoscale", "bwta_matmul_bool_prepared"]
+           "bwta_prepare_act_autoscale", "bwta_matmul_bool_prepared", "bwta_head_norm_rope", "bwta_cache_write", "bwta_cache_read",
+           "bwta_cache_attention", "bwta_cache_attention_workspace_bytes"]
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(
@@ -115,6 +116,26 @@ _lib.bwta_matmul_bool_prepared.argtypes = [_P, _c.c_int64, _P, _c.c_size_t, _c.c
                                            _P, _c.c_int, _c.c_float, _P, _c.c_int64, _c.c_int64, _P]
 _lib.bwta_prepare_act_autoscale.argtypes = [_P, _c.c_int64, _c.c_int, _c.c_int, _P, _P, _c.c_size_t,
                                             _c.POINTER(_c.c_int), _P]
+
+
+class Cache(_c.Structure):
+    """bwta_cache of bwta.h.  `tensors` keeps what the addresses point to alive (see make_cache)."""
+    _fields_ = [("k", _P), ("v", _P), ("k_scale", _P), ("v_scale", _P), ("blocks", _c.c_int32), ("kv_heads", _c.c_int32),
+                ("block", _c.c_int32), ("dim", _c.c_int32)]
+
+
+_CP = _c.POINTER(Cache)
+_lib.bwta_head_norm_rope.restype = _c.c_int
+_lib.bwta_head_norm_rope.argtypes = [_P, _c.c_int64, _c.c_int, _P, _P, _c.c_int64, _c.c_int, _P, _c.c_int, _c.c_int, _c.c_int, _c.c_int,
+                                     _c.c_float, _P, _P, _c.c_int, _c.c_int, _P, _c.c_int64, _P, _c.c_int64, _P]
+for _f in (_lib.bwta_cache_write, _lib.bwta_cache_read):
+    _f.restype = _c.c_int
+    _f.argtypes = [_CP, _P, _c.c_int64, _P, _c.c_int64, _c.c_int, _P, _c.c_int64, _P, _P, _c.c_int, _c.c_int, _c.c_int, _c.c_int, _P]
+_lib.bwta_cache_attention.restype = _c.c_int
+_lib.bwta_cache_attention.argtypes = [_CP, _P, _c.c_int64, _P, _c.c_int64, _c.c_int, _P, _P, _c.c_int64, _P, _P, _c.c_int, _c.c_int,
+                                      _c.c_int, _c.c_int, _c.c_int, _c.c_float, _c.c_int, _c.c_int, _P, _c.c_size_t, _P]
+_lib.bwta_cache_attention_workspace_bytes.restype = _c.c_size_t
+_lib.bwta_cache_attention_workspace_bytes.argtypes = [_c.c_int] * 7
 _lib.bwta_strerror.restype = _c.c_char_p
 _lib.bwta_strerror.argtypes = [_c.c_int]
 _lib.bwta_last_hip_error.restype = _c.c_int
@@ -403,6 +424,85 @@ def bwta_gemm_grouped(problem_array, workspace, *, M, N, K, a_scale_mode=SCALE_V
     ldo = N if ldo is None else ldo
     _check(_lib.bwta_gemm_grouped(problem_array, len(problem_array), M, N, K, a_scale_mode, w_scale_mode, ldo,
                                   _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream)))
+
+
+# ---- operators on heads ------------------------------------------------------------------------------
+
+
+def _dtype(x, dtype):
+    """The dtype argument of an operator on heads: as given, or the tensor's."""
+    if dtype is not None:
+        return dtype
+    try:
+        return {torch.float16: DTYPE_FP16, torch.bfloat16: DTYPE_BF16}[x.dtype]
+    except (AttributeError, KeyError):
+        raise TypeError("pass dtype= with addresses; tensors are float16 or bfloat16, got %s" % getattr(x, "dtype", type(x).__name__)) from None
+
+
+def make_cache(k, v, k_scale, v_scale, *, blocks=None, kv_heads=None, block=None, dim=None):
+    """The cache of 8-bit keys and values as the calls below take it (build once, reuse).  k [blocks, kv_heads, block, dim]
+    and v [blocks, kv_heads, dim, block] are contiguous tensors of one byte an element (uint8 or float8_e4m3fn), k_scale and
+    v_scale contiguous float32 [blocks, kv_heads]; or all four are addresses and the sizes are given.  The tensors are kept
+    alive."""
+    if not isinstance(k, int):
+        if k.dim() != 4:
+            raise ValueError("keys are [blocks, kv_heads, block, dim]")
+        sizes = tuple(k.shape)
+        for name, t, shape in (("k", k, sizes), ("v", v, (sizes[0], sizes[1], sizes[3], sizes[2])), ("k_scale", k_scale, sizes[:2]), ("v_scale", v_scale, sizes[:2])):
+            if tuple(t.shape) != shape or not t.is_contiguous() or t.device != k.device:
+                raise ValueError("%s has to be contiguous, of shape %s and on %s" % (name, shape, k.device))
+            if t.dtype not in ((torch.float32,) if "scale" in name else (torch.uint8, torch.float8_e4m3fn)):
+                raise TypeError("%s is %s" % (name, t.dtype))
+        given = (blocks, kv_heads, block, dim)
+        if any(g is not None and g != s for g, s in zip(given, sizes)):
+            raise ValueError("sizes %s given, the tensors have %s" % (given, sizes))
+        blocks, kv_heads, block, dim = sizes
+    c = Cache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), blocks, kv_heads, block, dim)
+    c.tensors = (k, v, k_scale, v_scale)
+    return c
+
+
+def bwta_head_norm_rope(Q, K, wq, wk, positions, inv_freq, Qout, Kout, *, M, heads, kv_heads, dim, rot_dim=None, eps=1e-6,
+                        norm=True, interleaved=False, ldq=None, ldk=None, ldqo=None, ldko=None, dtype=None, stream=None):
+    """rot_dim: all of dim unless given.  norm: whether heads are normalised (weights None: by 1)."""
+    ldq = heads * dim if ldq is None else ldq
+    ldk = kv_heads * dim if ldk is None else ldk
+    _check(_lib.bwta_head_norm_rope(_ptr(Q), ldq, heads, _ptr(wq), _ptr(K), ldk, kv_heads, _ptr(wk), _dtype(K if Q is None else Q, dtype),
+                                    M, dim, int(norm), eps, _ptr(positions), _ptr(inv_freq), dim if rot_dim is None else rot_dim, int(interleaved),
+                                    _ptr(Qout), heads * dim if ldqo is None else ldqo, _ptr(Kout), kv_heads * dim if ldko is None else ldko,
+                                    _stream(stream)))
+
+
+def _ldt(table, given):
+    if given is not None:
+        return given
+    return 0 if table is None or isinstance(table, int) else table.stride(0)
+
+
+def _cache_rows(call, cache, K, V, table, lens, cu, M, batch, max_new, max_len, ldk, ldv, ldt, dtype, stream):
+    width = cache.kv_heads * cache.dim
+    _check(call(cache, _ptr(K), width if ldk is None else ldk, _ptr(V), width if ldv is None else ldv, _dtype(K, dtype), _ptr(table),
+                _ldt(table, ldt), _ptr(lens), _ptr(cu), batch, M, max_new, max_len, _stream(stream)))
+
+
+def bwta_cache_write(cache, K, V, table, lens, cu=None, *, M, batch, max_new, max_len, ldk=None, ldv=None, ldt=None, dtype=None, stream=None):
+    _cache_rows(_lib.bwta_cache_write, cache, K, V, table, lens, cu, M, batch, max_new, max_len, ldk, ldv, ldt, dtype, stream)
+
+
+def bwta_cache_read(cache, K, V, table, lens, cu=None, *, M, batch, max_new, max_len, ldk=None, ldv=None, ldt=None, dtype=None, stream=None):
+    _cache_rows(_lib.bwta_cache_read, cache, K, V, table, lens, cu, M, batch, max_new, max_len, ldk, ldv, ldt, dtype, stream)
+
+
+def cache_attention_workspace_bytes(*, M, heads, kv_heads, dim, batch, max_new, max_len):
+    return int(_lib.bwta_cache_attention_workspace_bytes(M, heads, kv_heads, dim, batch, max_new, max_len))
+
+
+def bwta_cache_attention(cache, Q, out, lse, table, lens, cu=None, workspace=None, *, M, batch, max_new, max_len, heads, alpha, causal=True, window=0,
+                         ldq=None, ldo=None, ldt=None, dtype=None, workspace_bytes=None, stream=None):
+    width = heads * cache.dim
+    _check(_lib.bwta_cache_attention(cache, _ptr(Q), width if ldq is None else ldq, _ptr(out), width if ldo is None else ldo, _dtype(Q, dtype),
+                                     _ptr(lse), _ptr(table), _ldt(table, ldt), _ptr(lens), _ptr(cu), batch, M, max_new, max_len, heads, alpha,
+                                     int(causal), window, _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream)))
 
 
 def _native_identity():

@@ -5,8 +5,10 @@
 
 #include <string.h>
 #include <atomic>
+#include <cmath>
 #include <mutex>
 
+#include "bwta_heads.h"
 #include "bwta_internal.h"
 
 // Scratch of the entry point that allocates nothing (bwta_linear_static): part of the library's
@@ -534,6 +536,146 @@ int bwta_act_scale(const void *A, int64_t lda, int M, int K, void *s, bwta_strea
     return hip_result(bwta::launch_act_scale(A, lda, M, K, (uint16_t *)s, (hipStream_t)stream));
 }
 
+// ---- operators on heads ---------------------------------------------------------------------------
+
+// A launch's grid times 256 threads has to stay below 2^32.
+static constexpr double kMostGroups = (1 << 24) - 1;
+static constexpr int kMostHeads = 1 << 14;  // keeps every product of sizes in range
+
+static int check_rows(const void *p, int64_t ld, int heads, int dim)
+{
+    if (ld < (int64_t)heads * dim) return BWTA_ERR_SHAPE;
+    if (!p) return BWTA_ERR_NULL;
+    return aligned(p, 16) && ld % 8 == 0 ? BWTA_OK : BWTA_ERR_ALIGN;
+}
+
+// results must be rows of their own, or exactly those of the operand they are made from
+static bool rows_clash(const void *a, int64_t lda, int a_heads, const void *out, int64_t ldo, int o_heads, int M, int dim, bool may_be_same)
+{
+    if (may_be_same && a == out && lda == ldo) return false;
+    return rows_overlap(a, lda, a_heads * dim, out, ldo, o_heads * dim, M);
+}
+
+int bwta_head_norm_rope(const void *Q, int64_t ldq, int heads, const void *wq, const void *K, int64_t ldk, int kv_heads,
+                        const void *wk, int dtype, int M, int dim, int norm, float eps, const int32_t *positions,
+                        const float *inv_freq, int rot_dim, int interleaved, void *Qout, int64_t ldqo, void *Kout,
+                        int64_t ldko, bwta_stream_t stream)
+{
+    if (dtype != BWTA_DTYPE_FP16 && dtype != BWTA_DTYPE_BF16) return BWTA_ERR_UNSUPPORTED;
+    if (dim <= 0 || dim > 256 || dim % 16 || rot_dim < 0 || rot_dim > dim || rot_dim % 16) return BWTA_ERR_UNSUPPORTED;
+    if (norm && !(eps >= 0.0f && std::isfinite(eps))) return BWTA_ERR_UNSUPPORTED;
+    if (M < 0 || heads < 0 || kv_heads < 0) return BWTA_ERR_SHAPE;
+    if (heads > kMostHeads || kv_heads > kMostHeads || M > (1 << 25)) return BWTA_ERR_TOO_LARGE;
+    if (M == 0 || heads + kv_heads == 0) return BWTA_OK;
+    int rc;
+    if (heads && ((rc = check_rows(Q, ldq, heads, dim)) || (rc = check_rows(Qout, ldqo, heads, dim)))) return rc;
+    if (kv_heads && ((rc = check_rows(K, ldk, kv_heads, dim)) || (rc = check_rows(Kout, ldko, kv_heads, dim)))) return rc;
+    if (rot_dim && (!positions || !inv_freq)) return BWTA_ERR_NULL;
+    if (rot_dim && (!aligned(positions, 4) || !aligned(inv_freq, 4))) return BWTA_ERR_ALIGN;
+    if (norm && ((heads && !aligned(wq, 16)) || (kv_heads && !aligned(wk, 16)))) return BWTA_ERR_ALIGN;
+    if (heads && rows_clash(Q, ldq, heads, Qout, ldqo, heads, M, dim, true)) return BWTA_ERR_UNSUPPORTED;
+    if (kv_heads && rows_clash(K, ldk, kv_heads, Kout, ldko, kv_heads, M, dim, true)) return BWTA_ERR_UNSUPPORTED;
+    if (heads && kv_heads && (rows_clash(Q, ldq, heads, Kout, ldko, kv_heads, M, dim, false) || rows_clash(K, ldk, kv_heads, Qout, ldqo, heads, M, dim, false) ||
+                              rows_clash(Qout, ldqo, heads, Kout, ldko, kv_heads, M, dim, false)))
+        return BWTA_ERR_UNSUPPORTED;
+    const bwta::HeadRopeArgs a{{Q, K}, {Qout, Kout}, {norm ? wq : nullptr, norm ? wk : nullptr}, {ldq, ldk}, {ldqo, ldko}, {heads, kv_heads},
+                               M, dim, rot_dim, norm != 0, interleaved != 0, dtype == BWTA_DTYPE_BF16, eps, positions, inv_freq};
+    return hip_result(bwta::launch_head_norm_rope(a, (hipStream_t)stream));
+}
+
+// the cache and the sequences of a call; *none: nothing to do
+static int check_cache_call(const bwta_cache *c, int dtype, const int32_t *table, int64_t ldt, const int32_t *lens, const int32_t *cu, int batch,
+                            int M, int max_new, int max_len, bool *none)
+{
+    *none = false;
+    if (!c) return BWTA_ERR_NULL;
+    if (dtype != BWTA_DTYPE_FP16 && dtype != BWTA_DTYPE_BF16) return BWTA_ERR_UNSUPPORTED;
+    if (c->block != 64 && c->block != 128 && c->block != 256) return BWTA_ERR_UNSUPPORTED;
+    if (c->dim != 64 && c->dim != 128 && c->dim != 256) return BWTA_ERR_UNSUPPORTED;
+    if (c->blocks <= 0 || c->kv_heads <= 0 || batch < 0 || M < 0 || max_new < 0 || max_len < 0) return BWTA_ERR_SHAPE;
+    if (c->kv_heads > kMostHeads) return BWTA_ERR_TOO_LARGE;
+    if (!cu && (int64_t)batch * max_new > M) return BWTA_ERR_SHAPE;
+    if (ldt < ((int64_t)max_len + c->block - 1) / c->block) return BWTA_ERR_SHAPE;
+    if (M == 0 || batch == 0 || max_new == 0) {
+        *none = true;
+        return BWTA_OK;
+    }
+    if (!lens || (max_len && !table)) return BWTA_ERR_NULL;
+    if (!c->k || !c->v || !c->k_scale || !c->v_scale) return BWTA_ERR_NULL;
+    if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->k_scale, 4) || !aligned(c->v_scale, 4)) return BWTA_ERR_ALIGN;
+    if (!aligned(table, 4) || !aligned(lens, 4) || !aligned(cu, 4)) return BWTA_ERR_ALIGN;
+    return BWTA_OK;
+}
+
+static bwta::CacheArgs cache_args(const bwta_cache *c)
+{
+    return {(uint8_t *)c->k, (uint8_t *)c->v, c->k_scale, c->v_scale, c->blocks, c->kv_heads, c->block, c->dim};
+}
+
+static int check_cache_rows(const bwta_cache *c, const void *K, int64_t ldk, const void *V, int64_t ldv, const bwta::SeqArgs &s)
+{
+    int rc;
+    if ((rc = check_rows(K, ldk, c->kv_heads, c->dim)) || (rc = check_rows(V, ldv, c->kv_heads, c->dim))) return rc;
+    return bwta::cache_rows_groups(cache_args(c), s) > kMostGroups ? BWTA_ERR_TOO_LARGE : BWTA_OK;
+}
+
+int bwta_cache_write(const bwta_cache *cache, const void *K, int64_t ldk, const void *V, int64_t ldv, int dtype,
+                     const int32_t *table, int64_t ldt, const int32_t *lens, const int32_t *cu, int batch, int M,
+                     int max_new, int max_len, bwta_stream_t stream)
+{
+    bool none;
+    int rc = check_cache_call(cache, dtype, table, ldt, lens, cu, batch, M, max_new, max_len, &none);
+    if (rc != BWTA_OK || none) return rc;
+    const bwta::SeqArgs s{table, ldt, lens, cu, batch, M, max_new, max_len};
+    if ((rc = check_cache_rows(cache, K, ldk, V, ldv, s))) return rc;
+    return hip_result(bwta::launch_cache_write({cache_args(cache), s, K, V, ldk, ldv, dtype == BWTA_DTYPE_BF16}, (hipStream_t)stream));
+}
+
+int bwta_cache_read(const bwta_cache *cache, void *K, int64_t ldk, void *V, int64_t ldv, int dtype, const int32_t *table,
+                    int64_t ldt, const int32_t *lens, const int32_t *cu, int batch, int M, int max_new, int max_len,
+                    bwta_stream_t stream)
+{
+    bool none;
+    int rc = check_cache_call(cache, dtype, table, ldt, lens, cu, batch, M, max_new, max_len, &none);
+    if (rc != BWTA_OK || none) return rc;
+    const bwta::SeqArgs s{table, ldt, lens, cu, batch, M, max_new, max_len};
+    if ((rc = check_cache_rows(cache, K, ldk, V, ldv, s))) return rc;
+    if (rows_clash(K, ldk, cache->kv_heads, V, ldv, cache->kv_heads, M, cache->dim, false)) return BWTA_ERR_UNSUPPORTED;
+    return hip_result(bwta::launch_cache_read({cache_args(cache), s, K, V, ldk, ldv, dtype == BWTA_DTYPE_BF16}, (hipStream_t)stream));
+}
+
+size_t bwta_cache_attention_workspace_bytes(int M, int heads, int kv_heads, int dim, int batch, int max_new, int max_len)
+{
+    if (M <= 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || heads > kMostHeads || dim <= 0 || dim > 256 || batch <= 0 || max_new <= 0 || max_len <= 0) return 0;
+    const int splits = bwta::cache_attention_splits(batch, heads, kv_heads, dim, max_new, max_len);
+    return splits > 1 ? round_up((size_t)splits * M * heads * (dim + 2) * sizeof(float), 256) : 0;
+}
+
+int bwta_cache_attention(const bwta_cache *cache, const void *Q, int64_t ldq, void *out, int64_t ldo, int dtype, float *lse,
+                         const int32_t *table, int64_t ldt, const int32_t *lens, const int32_t *cu, int batch, int M,
+                         int max_new, int max_len, int heads, float alpha, int causal, int window, void *workspace,
+                         size_t workspace_bytes, bwta_stream_t stream)
+{
+    bool none;
+    int rc = check_cache_call(cache, dtype, table, ldt, lens, cu, batch, M, max_new, max_len, &none);
+    if (rc != BWTA_OK) return rc;
+    if (heads <= 0 || heads % cache->kv_heads) return BWTA_ERR_SHAPE;
+    if (heads > kMostHeads) return BWTA_ERR_TOO_LARGE;
+    if (!(alpha > 0.0f && std::isfinite(alpha)) || window < 0 || (window && !causal)) return BWTA_ERR_UNSUPPORTED;
+    if (none) return BWTA_OK;
+    if ((rc = check_rows(Q, ldq, heads, cache->dim)) || (rc = check_rows(out, ldo, heads, cache->dim))) return rc;
+    if (lse && !aligned(lse, 4)) return BWTA_ERR_ALIGN;
+    if (rows_clash(Q, ldq, heads, out, ldo, heads, M, cache->dim, true)) return BWTA_ERR_UNSUPPORTED;
+    const size_t need = bwta_cache_attention_workspace_bytes(M, heads, cache->kv_heads, cache->dim, batch, max_new, max_len);
+    if (need && (!workspace || workspace_bytes < need)) return BWTA_ERR_WORKSPACE;
+    if (need && !aligned(workspace, 256)) return BWTA_ERR_ALIGN;
+    const bwta::SeqArgs s{table, ldt, lens, cu, batch, M, max_new, max_len};
+    const int splits = need ? bwta::cache_attention_splits(batch, heads, cache->kv_heads, cache->dim, max_new, max_len) : 1;
+    if (bwta::cache_attention_groups(batch, heads, cache->kv_heads, cache->dim, max_new, splits) > kMostGroups) return BWTA_ERR_TOO_LARGE;
+    return hip_result(bwta::launch_cache_attention({cache_args(cache), s, Q, out, ldq, ldo, lse, heads, alpha, causal != 0, dtype == BWTA_DTYPE_BF16, window,
+                                                    (float *)workspace, splits}, (hipStream_t)stream));
+}
+
 const char *bwta_strerror(int code)
 {
     switch (code) {
@@ -541,10 +683,10 @@ const char *bwta_strerror(int code)
     case BWTA_ERR_NULL: return "a required pointer is NULL";
     case BWTA_ERR_SHAPE: return "invalid shape or leading dimension";
     case BWTA_ERR_ALIGN: return "misaligned pointer";
-    case BWTA_ERR_UNSUPPORTED: return "unsupported dtype, scale mode or path";
+    case BWTA_ERR_UNSUPPORTED: return "unsupported dtype, scale mode, path or parameter";
     case BWTA_ERR_WORKSPACE: return "workspace missing or too small";
     case BWTA_ERR_HIP: return "HIP runtime error at launch (see bwta_last_hip_error)";
-    case BWTA_ERR_TOO_LARGE: return "the shape needs more scratch than the library's static scratch holds";
+    case BWTA_ERR_TOO_LARGE: return "the shape needs more than the library's static scratch, or than one launch, holds";
     default: return "unknown error code";
     }
 }
@@ -636,7 +778,7 @@ int bwta_planned_decode_blocks(int M, int N, int K, int count)
     return plan_from_planes(g, true) == BWTA_KERNEL_GEMV_FP4 ? bwta::gemv_fp4_planned_blocks(M, N, K, count) : 0;
 }
 
-int bwta_version(void) { return 2; }
+int bwta_version(void) { return 3; }
 
 #ifndef BWTA_BUILD_ID
 #define BWTA_BUILD_ID "unknown"
