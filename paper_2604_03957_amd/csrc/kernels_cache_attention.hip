@@ -21,6 +21,7 @@ typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf2v __attribute__((ext_vector_type(2)));
 typedef float float4v __attribute__((ext_vector_type(4)));
+typedef float float16v __attribute__((ext_vector_type(16)));
 
 template <typename T> struct Mma;
 template <> struct Mma<_Float16> {
@@ -30,6 +31,7 @@ template <> struct Mma<_Float16> {
         return hi ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, 1.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, 1.0f, false);
     }
     static __device__ __forceinline__ float4v mma(half8 a, half8 b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ float16v mma(half8 a, half8 b, float16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
 template <> struct Mma<__bf16> {
     typedef bf8 Frag;
@@ -38,6 +40,7 @@ template <> struct Mma<__bf16> {
         return hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.0f, false);
     }
     static __device__ __forceinline__ float4v mma(bf8 a, bf8 b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ float16v mma(bf8 a, bf8 b, float16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 };
 
 // eight codes as a matrix-core operand's eight values
@@ -64,6 +67,22 @@ __device__ __forceinline__ float sum_of_query(float x)
     return x + __shfl_xor(x, 32);
 }
 
+// Four channels of a row, and once per row its maximum (as a power of two) and sum: the result, or this split's part of it.
+template <typename T, int D>
+__device__ __forceinline__ void give(const CacheAttentionArgs &a, const Seq &s, int head, int group, int split, int64_t row, int channel, float4v x, float m, float l, bool once)
+{
+    const int64_t token = s.row + row / group, at = token * a.heads + head * group + row % group;
+    if (a.splits > 1) {
+        const int64_t all_rows = (int64_t)a.seq.M * a.heads;
+        *(float4v *)(a.partial + (split * all_rows + at) * D + channel) = x;
+        if (once) ((float2 *)(a.partial + a.splits * all_rows * D))[split * all_rows + at] = make_float2(m, l);
+        return;
+    }
+    const float f = l == 0.0f ? 0.0f : 1.0f / l;
+    *(uint2 *)((T *)a.out + token * a.ldo + (head * group + row % group) * D + channel) = make_uint2(Half<T>::pack(x[0] * f, x[1] * f), Half<T>::pack(x[2] * f, x[3] * f));
+    if (once && a.lse) a.lse[at] = kLn2 * (m + log2f(l));
+}
+
 // Rows of one sequence and key head: row r is query head r % group of the r / group-th new token.  A wavefront has NB * 16
 // of them.  SHARED: the WAVES wavefronts of a workgroup have the same rows and take turns at the steps of 64 keys; else
 // each has rows of its own and they all walk the same keys.
@@ -74,7 +93,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_cache_attention(CacheAttentionAr
     typedef typename Mma<T>::Frag Frag;
     __shared__ float4 merged[SHARED ? WAVES * R * (D / 4) : 1];
     __shared__ float2 merged_ml[SHARED ? WAVES * R : 1];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q16 = lane & 15, g = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q16 = lane & 15, g = lane >> 4;
     const int H = a.cache.heads, group = a.heads / H;
 
     unsigned i = blockIdx.x;
@@ -242,23 +261,6 @@ __global__ __launch_bounds__(WAVES * 64) void k_cache_attention(CacheAttentionAr
 #pragma unroll
         for (int n = 0; n < NV; ++n) o[nb][n] *= unit;
     }
-    const int64_t all_rows = (int64_t)a.seq.M * a.heads;
-    float *const part_o = a.partial + (int64_t)split * all_rows * D;
-    float2 *const part_ml = (float2 *)(a.partial + a.splits * all_rows * D) + split * all_rows;
-
-    // four channels of a row, and once per row its maximum (as a power of two) and sum
-    auto give = [&](int64_t row, int channel, float4v x, float m_, float l_, bool once) {
-        const int64_t token = s.row + row / group;
-        const int h = head * group + (int)(row % group);
-        if (a.splits > 1) {
-            *(float4v *)(part_o + (token * a.heads + h) * D + channel) = x;
-            if (once) part_ml[token * a.heads + h] = make_float2(m_, l_);
-            return;
-        }
-        const float f = l_ == 0.0f ? 0.0f : 1.0f / l_;
-        *(uint2 *)((T *)a.out + token * a.ldo + (int64_t)h * D + channel) = make_uint2(Half<T>::pack(x[0] * f, x[1] * f), Half<T>::pack(x[2] * f, x[3] * f));
-        if (once && a.lse) a.lse[token * a.heads + h] = kLn2 * (m_ + log2f(l_));
-    };
     if constexpr (SHARED) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
@@ -283,51 +285,289 @@ __global__ __launch_bounds__(WAVES * 64) void k_cache_attention(CacheAttentionAr
                 x += float4v{y.x, y.y, y.z, y.w} * f;
                 sum = fmaf(ml.y, f, sum);
             }
-            give(first + r, at % (D / 4) * 4, x, top, sum, at % (D / 4) == 0);
-        }
-    } else {
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            const int64_t row = first + wave * R + nb * 16 + q16;
-            if (row >= total) continue;
-#pragma unroll
-            for (int n = 0; n < NV; ++n) give(row, 16 * n + 4 * g, o[nb][n], m[nb], l[nb], n == 0 && g == 0);
+            give<T, D>(a, s, head, group, split, first + r, at % (D / 4) * 4, x, top, sum, at % (D / 4) == 0);
         }
     }
 }
 
-// The parts of one row side by side: a wavefront per row.
+// Many rows: each wavefront has NB * 32 of its own, and a workgroup's wavefronts share the keys and values of a step, which
+// reach LDS as 16-bit numbers (each code is widened once for the workgroup, not once for each wavefront), two steps' worth:
+// one is computed with while the next arrives.  Products of 32 x 32: key row 8 i + 4 j + r of a block of 32 is token
+// 16 j + 4 i + r, so a lane again has 16 tokens in a row.  16-byte chunks of a row are swapped by the row's last three bits,
+// which spreads the eight rows that are read at a time over the banks.
+template <typename T, int D, int NB, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_cache_attention_rows(CacheAttentionArgs a, int row_tiles)
+{
+    constexpr int R = 32 * NB, kRows = R * WAVES, NT = WAVES * 64, KK = D / 16, DN = D / 32, kUnits = 4 * D / NT;
+    typedef typename Mma<T>::Frag Frag;
+    __shared__ uint4 keys[2][kCacheTile * D / 8], values[2][kCacheTile * D / 8];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), q32 = lane & 31, h2 = lane >> 5;
+    const int H = a.cache.heads, group = a.heads / H;
+
+    unsigned i = blockIdx.x;
+    const int split = i % a.splits;
+    i /= a.splits;
+    const int bh = i % (a.seq.batch * H), head = bh % H, b = bh / H;
+    const int tile_of_rows = row_tiles - 1 - (int)(i / (a.seq.batch * H));  // causal rows at the end see most: first
+    const Seq s = sequence(a.seq, b);
+    const int64_t total = (int64_t)s.n * group;
+    const int64_t first = (int64_t)tile_of_rows * kRows;
+    if (first >= total) return;
+
+    // keys that some row of rows [lo, lo + count) sees, and those that every one sees
+    struct Span {
+        int begin, end, all_begin, all_end;
+    };
+    auto span = [&](int64_t lo, int count) {
+        const int64_t hi = min(lo + count, total) - 1;
+        const int t0 = (int)(lo / group), t1 = (int)(hi / group);
+        Span r;
+        r.end = hi < lo ? 0 : a.causal ? max(0, min(s.len, s.start + t1 + 1)) : s.len;
+        r.begin = a.window ? max(0, s.start + t0 - a.window + 1) : 0;
+        r.all_end = a.causal ? min(s.len, s.start + t0 + 1) : s.len;
+        r.all_begin = a.window ? s.start + t1 - a.window + 1 : 0;
+        return r;
+    };
+    const Span whole = span(first, kRows), mine = span(first + wave * R, R);
+    const int step0 = whole.begin / kCacheTile, steps = max(0, (whole.end + kCacheTile - 1) / kCacheTile - step0);
+    const int from = step0 + (int)((int64_t)steps * split / a.splits), to = step0 + (int)((int64_t)steps * (split + 1) / a.splits);
+
+    int see_lo[NB], see_hi[NB];
+    Frag q[NB][KK];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+        const int64_t row = first + wave * R + nb * 32 + q32;
+        const bool has = row < total;
+        const int t = has ? (int)(row / group) : 0, h = head * group + (has ? (int)(row % group) : 0);
+        see_hi[nb] = !has ? -1 : a.causal ? min(s.len - 1, s.start + t) : s.len - 1;
+        see_lo[nb] = a.window ? s.start + t - a.window + 1 : 0;
+        const T *x = (const T *)a.q + (s.row + t) * a.ldq + (int64_t)h * D;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+            if (has) q[nb][kk] = *(const Frag *)(x + 16 * kk + 8 * h2);
+            else q[nb][kk] = Frag{};
+        }
+    }
+
+    float16v o[NB][DN] = {};
+    float m[NB], l[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) m[nb] = -INFINITY, l[nb] = 0.0f;
+    int eref = 0;
+    bool begun = false;
+    const int per_block = a.cache.block / kCacheTile;
+
+    uint4 kc[kUnits], vc[kUnits];  // the next step's codes
+    float ks_next;
+    int ev_next;
+    bool ok_next;
+    auto fetch = [&](int step) {
+        const int ordinal = step / per_block, sub = step - ordinal * per_block;
+        int page = a.seq.table[b * a.seq.ldt + ordinal];
+        ok_next = page >= 0 && page < a.cache.blocks;
+        if (!ok_next) page = 0;
+        const int64_t unit = (int64_t)page * H + head;
+        const uint8_t *kp = a.cache.k + (unit * a.cache.block + sub * kCacheTile) * D;
+        const uint8_t *vp = a.cache.v + unit * D * a.cache.block + sub * kCacheTile;
+        ks_next = a.cache.k_scale[unit];
+        ev_next = exponent_of(a.cache.v_scale[unit]);
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const int at = tid + u * NT;
+            kc[u] = *(const uint4 *)(kp + 16 * at);
+            vc[u] = *(const uint4 *)(vp + (int64_t)(at >> 2) * a.cache.block + 16 * (at & 3));
+        }
+    };
+    auto stage = [&](int step, int buffer) {
+        // a slot behind the sequence holds anything, a NaN too: its weight 0 does not hide that
+        const bool tail = !ok_next || (step + 1) * kCacheTile > s.len;
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const int at = tid + u * NT, token = at / KK, c = 2 * (at % KK);
+            const int row = (token & 32) + 8 * (token >> 2 & 3) + 4 * (token >> 4 & 1) + (token & 3);
+            union {
+                Frag f;
+                uint4 w;
+            } x, y;
+            x.f = widen<T>(kc[u].x, kc[u].y), y.f = widen<T>(kc[u].z, kc[u].w);
+            keys[buffer][row * (D / 8) + (c ^ (row & 7))] = x.w;
+            keys[buffer][row * (D / 8) + ((c + 1) ^ (row & 7))] = y.w;
+            const int d = at >> 2, cv = 2 * (at & 3);
+            uint4 codes = vc[u];
+            if (tail) {
+                const int valid = ok_next ? s.len - step * kCacheTile - 16 * (at & 3) : 0;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int bytes = min(max(valid - 4 * w, 0), 4);
+                    (&codes.x)[w] &= bytes == 4 ? 0xffffffffu : (1u << (8 * bytes)) - 1;
+                }
+            }
+            union {
+                half8 f;
+                uint4 w;
+            } v, z;
+            v.f = widen<_Float16>(codes.x, codes.y), z.f = widen<_Float16>(codes.z, codes.w);
+            values[buffer][d * 8 + (cv ^ (d & 7))] = v.w;
+            values[buffer][d * 8 + ((cv + 1) ^ (d & 7))] = z.w;
+        }
+    };
+
+    if (from < to) {
+        fetch(from);
+        stage(from, 0);
+    }
+    for (int step = from; step < to; ++step) {
+        const int buffer = (step - from) & 1;
+        const float ks = ks_next;
+        const int ev = ev_next;
+        const bool ok = ok_next;
+        __syncthreads();
+        if (step + 1 < to) fetch(step + 1);
+        if (ok && step * kCacheTile < mine.end && (step + 1) * kCacheTile > mine.begin) {  // else no row of this wavefront sees any of these keys
+            float16v sc[NB][2] = {};
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk) {
+                    const int row = 32 * kb + q32;
+                    const Frag f = *(const Frag *)&keys[buffer][row * (D / 8) + ((2 * kk + h2) ^ (row & 7))];
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) sc[nb][kb] = Mma<T>::mma(f, q[nb][kk], sc[nb][kb]);
+                }
+            if ((step + 1) * kCacheTile > mine.all_end || step * kCacheTile < mine.all_begin) {
+                const int key0 = step * kCacheTile + 16 * h2;
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const int key = key0 + 32 * kb + r;
+                            sc[nb][kb][r] = ((key > see_hi[nb]) | (key < see_lo[nb])) ? -INFINITY : sc[nb][kb][r];
+                        }
+            }
+            const float c = fmaxf(a.alpha * kLog2e * ks, 1.17549435e-38f);
+            if (!begun) eref = ev, begun = true;
+            if (ev - eref > kDrift || eref - ev > kDrift) {
+                const float f = pow2(eref - ev);
+                eref = ev;
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int n = 0; n < DN; ++n) o[nb][n] *= f;
+            }
+            const float drift = (float)(ev - eref), undrift = pow2(eref - ev);
+            half8 p[NB][4];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                float top = -INFINITY;
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int r = 0; r < 16; r += 2) top = fmaxf(top, fmaxf(sc[nb][kb][r], sc[nb][kb][r + 1]));
+                top *= c;
+                if (__any(top > m[nb] + kSlack)) {
+                    const float now = fmaxf(m[nb], fmaxf(top, __shfl_xor(top, 32)));
+                    const float f = m[nb] == -INFINITY ? 0.0f : exp2f(m[nb] - now);
+                    m[nb] = now;
+                    l[nb] *= f;
+#pragma unroll
+                    for (int n = 0; n < DN; ++n) o[nb][n] *= f;
+                }
+                const float base = (m[nb] == -INFINITY ? 0.0f : m[nb]) - drift;
+                float sum[4] = {};
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int hf = 0; hf < 2; ++hf) {
+                        float w[8];
+#pragma unroll
+                        for (int r = 0; r < 8; ++r) {
+                            w[r] = __builtin_amdgcn_exp2f(fmaf(sc[nb][kb][8 * hf + r], c, -base));
+                            sum[r & 3] += w[r];
+                        }
+                        p[nb][2 * kb + hf] = half8{(_Float16)w[0], (_Float16)w[1], (_Float16)w[2], (_Float16)w[3], (_Float16)w[4], (_Float16)w[5], (_Float16)w[6], (_Float16)w[7]};
+                    }
+                l[nb] = fmaf((sum[0] + sum[1]) + (sum[2] + sum[3]), undrift, l[nb]);
+            }
+#pragma unroll
+            for (int n = 0; n < DN; ++n)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const int d = 32 * n + q32;
+                    const half8 f = *(const half8 *)&values[buffer][d * 8 + ((4 * (t >> 1) + 2 * h2 + (t & 1)) ^ (d & 7))];
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) o[nb][n] = Mma<_Float16>::mma(f, p[nb][t], o[nb][n]);
+                }
+        }
+        if (step + 1 < to) stage(step + 1, buffer ^ 1);
+    }
+
+    // o[nb][n][r]: query q32 of the nb-th 32, channel 32 n + 8 (r / 4) + 4 h2 + r % 4, in units of 2^eref
+    const float unit = pow2(eref);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+        const float sum = l[nb] + __shfl_xor(l[nb], 32);
+        const int64_t row = first + wave * R + nb * 32 + q32;
+        if (row >= total) continue;
+#pragma unroll
+        for (int n = 0; n < DN; ++n)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                give<T, D>(a, s, head, group, split, row, 32 * n + 8 * r + 4 * h2, float4v{o[nb][n][4 * r], o[nb][n][4 * r + 1], o[nb][n][4 * r + 2], o[nb][n][4 * r + 3]} * unit,
+                           m[nb], sum, n == 0 && r == 0 && h2 == 0);
+    }
+}
+
+// The parts of one row: a workgroup per row, some threads for each four channels.
+constexpr int kMostSplits = 128;
 template <typename T, int D>
 __global__ __launch_bounds__(256) void k_cache_attention_join(CacheAttentionArgs a)
 {
-    constexpr int C = D / 64;
-    const int lane = threadIdx.x & 63;
-    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int h = (int)(item % a.heads);
-    const int64_t bt = item / a.heads;
+    constexpr int C = D / 4, kSide = 256 / C;  // parts side by side
+    __shared__ float weight[kMostSplits], total[2];
+    __shared__ float4v side[kSide][C];
+    const int tid = threadIdx.x, h = (int)(blockIdx.x % a.heads);
+    const unsigned bt = blockIdx.x / a.heads;
     const int b = (int)(bt / a.seq.max_new), t = (int)(bt % a.seq.max_new);
-    if (b >= a.seq.batch) return;
     const Seq s = sequence(a.seq, b);
     if (t >= s.n) return;
     const int64_t all_rows = (int64_t)a.seq.M * a.heads, row = (int64_t)(s.row + t) * a.heads + h;
-    const float2 *ml = (const float2 *)(a.partial + a.splits * all_rows * D) + row;
-    const float *o = a.partial + row * D + lane * C;
-    float top = -INFINITY;
-    for (int k = 0; k < a.splits; ++k) top = fmaxf(top, ml[k * all_rows].x);
-    float sum = 0.0f, x[C] = {};
-    for (int k = 0; k < a.splits; ++k) {
-        const float2 p = ml[k * all_rows];
-        if (p.x == -INFINITY && p.y == 0.0f) continue;
-        const float f = exp2f(p.x - top);
-        sum = fmaf(p.y, f, sum);
+    if (tid < 64) {
+        const float2 *ml = (const float2 *)(a.partial + a.splits * all_rows * D) + row;
+        float2 p[kMostSplits / 64];
+        float top = -INFINITY, sum = 0.0f;
 #pragma unroll
-        for (int c = 0; c < C; ++c) x[c] = fmaf(o[k * all_rows * D + c], f, x[c]);
+        for (int j = 0; j < kMostSplits / 64; ++j) {
+            p[j] = tid + 64 * j < a.splits ? ml[(tid + 64 * j) * all_rows] : make_float2(-INFINITY, 0.0f);
+            top = fmaxf(top, p[j].x);
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+#pragma unroll
+        for (int j = 0; j < kMostSplits / 64; ++j) {
+            const float f = p[j].x == -INFINITY && p[j].y == 0.0f ? 0.0f : exp2f(p[j].x - top);
+            weight[tid + 64 * j] = f;
+            sum = fmaf(f, p[j].y, sum);
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+        if (tid == 0) total[0] = top, total[1] = sum;
     }
-    const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
-    T *out = (T *)a.out + (s.row + t) * a.ldo + (int64_t)h * D + lane * C;
+    __syncthreads();
+    const int c = tid % C, first = tid / C;
+    const float *o = a.partial + row * D + 4 * c;
+    float4v x = {};
+#pragma unroll 4
+    for (int k = first; k < a.splits; k += kSide) x += *(const float4v *)(o + k * all_rows * D) * weight[k];
+    side[first][c] = x;
+    __syncthreads();
+    if (first) return;
 #pragma unroll
-    for (int c = 0; c < C; ++c) out[c] = (T)(x[c] * f);
-    if (lane == 0 && a.lse) a.lse[row] = kLn2 * (top + log2f(sum));
+    for (int k = 1; k < kSide; ++k) x += side[k][c];
+    const float sum = total[1], f = sum == 0.0f ? 0.0f : 1.0f / sum;
+    *(uint2 *)((T *)a.out + (s.row + t) * a.ldo + (int64_t)h * D + 4 * c) = make_uint2(Half<T>::pack(x[0] * f, x[1] * f), Half<T>::pack(x[2] * f, x[3] * f));
+    if (c == 0 && a.lse) a.lse[row] = kLn2 * (total[0] + log2f(sum));
 }
 
 // Rows a workgroup takes: up to 16 or 32 shared by four wavefronts, else 32 for each of four.
@@ -339,7 +579,7 @@ Shape shape_of(int64_t rows, int dim)
 {
     if (rows <= 16) return {16, true};
     if (rows <= 32 && dim < 256) return {32, true};
-    return {dim < 256 ? 128 : 64, false};
+    return {128, false};
 }
 constexpr int kAttWaves = 4;
 
@@ -349,14 +589,14 @@ void launch(const CacheAttentionArgs &a, const Shape &shape, int row_tiles, int6
     constexpr int NB = D < 256 ? 2 : 1;
     const dim3 grid((unsigned)groups), block(kAttWaves * 64);
     if (!shape.shared)
-        hipLaunchKernelGGL((k_cache_attention<T, D, NB, kAttWaves, false>), grid, block, 0, st, a, row_tiles);
+        hipLaunchKernelGGL((k_cache_attention_rows<T, D, 1, kAttWaves>), grid, block, 0, st, a, row_tiles);
     else if (shape.rows == 16)
         hipLaunchKernelGGL((k_cache_attention<T, D, 1, kAttWaves, true>), grid, block, 0, st, a, row_tiles);
     else
         hipLaunchKernelGGL((k_cache_attention<T, D, NB, kAttWaves, true>), grid, block, 0, st, a, row_tiles);
     if (a.splits > 1) {
         const int64_t rows = (int64_t)a.seq.batch * a.seq.max_new * a.heads;
-        hipLaunchKernelGGL((k_cache_attention_join<T, D>), dim3((unsigned)((rows + 3) / 4)), block, 0, st, a);
+        hipLaunchKernelGGL((k_cache_attention_join<T, D>), dim3((unsigned)rows), block, 0, st, a);
     }
 }
 
@@ -384,9 +624,10 @@ int cache_attention_splits(int batch, int heads, int kv_heads, int dim, int max_
     const double groups = cache_attention_groups(batch, heads, kv_heads, dim, max_new, 1);
     const int64_t steps = ((int64_t)max_len + kCacheTile - 1) / kCacheTile;
     // four workgroups for every compute unit, as long as each of their wavefronts still has a few steps
+    if (!shape.shared && groups >= 256) return 1;
     const int64_t want = groups >= 1024 ? 1 : (int64_t)((1024 + groups - 1) / groups), most = steps / (shape.shared ? kAttWaves : 4);
     const int64_t s = want < most ? want : most;
-    return (int)(s < 1 ? 1 : s > 128 ? 128 : s);
+    return (int)(s < 1 ? 1 : s > kMostSplits ? kMostSplits : s);
 }
 
 hipError_t launch_cache_attention(const CacheAttentionArgs &a, hipStream_t st)
