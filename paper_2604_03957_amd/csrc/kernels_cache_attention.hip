@@ -55,6 +55,9 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417
 constexpr float kSlack = 8.0f;  // weights may reach 2^kSlack before the maximum is moved
 constexpr int kDrift = 4;       // bits a block's value scale may differ from eref
 
+// The larger one; a NaN if either is one (which saves making a quiet one of it first).
+__device__ __forceinline__ float most(float x, float y) { return __builtin_elementwise_maximum(x, y); }
+
 // the same value for all four lanes that share a query (lane, lane ^ 16, lane ^ 32, lane ^ 48)
 __device__ __forceinline__ float max_of_query(float x)
 {
@@ -83,16 +86,15 @@ __device__ __forceinline__ void give(const CacheAttentionArgs &a, const Seq &s, 
     if (once && a.lse) a.lse[at] = kLn2 * (m + log2f(l));
 }
 
-// Rows of one sequence and key head: row r is query head r % group of the r / group-th new token.  A wavefront has NB * 16
-// of them.  SHARED: the WAVES wavefronts of a workgroup have the same rows and take turns at the steps of 64 keys; else
-// each has rows of its own and they all walk the same keys.
-template <typename T, int D, int NB, int WAVES, bool SHARED>
-__global__ __launch_bounds__(WAVES * 64) void k_cache_attention(CacheAttentionArgs a, int row_tiles)
+// Rows of one sequence and key head: row r is query head r % group of the r / group-th new token.  Here a workgroup has
+// NB * 16 of them, and its wavefronts take turns at the steps of 64 keys.
+template <typename T, int D, int NB, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_cache_attention(CacheAttentionArgs a, int row_tiles)
 {
-    constexpr int R = 16 * NB, kRows = SHARED ? R : R * WAVES, KL = D / 64, NV = D / 16;
+    constexpr int R = 16 * NB, KL = D / 64, NV = D / 16;
     typedef typename Mma<T>::Frag Frag;
-    __shared__ float4 merged[SHARED ? WAVES * R * (D / 4) : 1];
-    __shared__ float2 merged_ml[SHARED ? WAVES * R : 1];
+    __shared__ float4 merged[WAVES * R * (D / 4)];
+    __shared__ float2 merged_ml[WAVES * R];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q16 = lane & 15, g = lane >> 4;
     const int H = a.cache.heads, group = a.heads / H;
 
@@ -103,9 +105,9 @@ __global__ __launch_bounds__(WAVES * 64) void k_cache_attention(CacheAttentionAr
     const int tile_of_rows = row_tiles - 1 - (int)(i / (a.seq.batch * H));  // causal rows at the end see most: first
     const Seq s = sequence(a.seq, b);
     const int64_t total = (int64_t)s.n * group;
-    const int64_t first = (int64_t)tile_of_rows * kRows;
+    const int64_t first = (int64_t)tile_of_rows * R;
     if (first >= total) return;
-    const int64_t last = min(first + kRows, total) - 1;
+    const int64_t last = min(first + R, total) - 1;
 
     // keys that some row sees, and those that every row sees
     const int t_first = (int)(first / group), t_last = (int)(last / group);
@@ -120,7 +122,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_cache_attention(CacheAttentionAr
     Frag q[NB][2 * KL];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-        const int64_t row = first + (SHARED ? 0 : wave * R) + nb * 16 + q16;
+        const int64_t row = first + nb * 16 + q16;
         const bool has = row < total;
         const int t = has ? (int)(row / group) : 0, h = head * group + (has ? (int)(row % group) : 0);
         see_hi[nb] = !has ? -1 : a.causal ? min(s.len - 1, s.start + t) : s.len - 1;
@@ -141,26 +143,48 @@ __global__ __launch_bounds__(WAVES * 64) void k_cache_attention(CacheAttentionAr
     for (int nb = 0; nb < NB; ++nb) m[nb] = -INFINITY, l[nb] = 0.0f;
     int eref = 0;
     bool begun = false;
-    const int per_block = a.cache.block / kCacheTile;
+    const int block_shift = a.cache.block >> 7;  // 64, 128, 256 tokens: 1, 2, 4 steps
     const int key_row = 16 * (q16 >> 2) + (q16 & 3);  // + 4 b
 
-    for (int step = from + (SHARED ? wave : 0); step < to; step += SHARED ? WAVES : 1) {
-        const int ordinal = step / per_block, sub = step - ordinal * per_block;
-        int page = a.seq.table[b * a.seq.ldt + ordinal];
-        const bool page_ok = page >= 0 && page < a.cache.blocks;
-        if (!page_ok) page = 0;
+    // Loads run ahead of what waits for them: a step's codes and scales are asked for one turn before, its block two turns
+    // before (the address depends on it).
+    uint4 kc[4][KL], vc[NV], kn[4][KL], vn[NV];
+    float ks_next = 0.0f, vs_next = 0.0f;
+    bool ok_next = false;
+    int page_next = -1;
+    auto page_of = [&](int step) { return a.seq.table[b * a.seq.ldt + (min(step, to - 1) >> block_shift)]; };
+    auto fetch = [&](int step) {
+        const int sub = step & ((1 << block_shift) - 1);
+        int page = __builtin_amdgcn_readfirstlane(page_next);
+        ok_next = page >= 0 && page < a.cache.blocks;
+        if (!ok_next) page = 0;
         const int64_t unit = (int64_t)page * H + head;
         const uint8_t *kp = a.cache.k + (unit * a.cache.block + sub * kCacheTile) * D;
         const uint8_t *vp = a.cache.v + unit * D * a.cache.block + sub * kCacheTile;
-        const float ks = a.cache.k_scale[unit];
-        const int ev = exponent_of(a.cache.v_scale[unit]);
-        uint4 kc[4][KL], vc[NV];
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
-            for (int j = 0; j < KL; ++j) kc[kb][j] = *(const uint4 *)(kp + (key_row + 4 * kb) * D + 64 * j + 16 * g);
+            for (int j = 0; j < KL; ++j) kn[kb][j] = *(const uint4 *)(kp + (key_row + 4 * kb) * D + 64 * j + 16 * g);
+        ks_next = a.cache.k_scale[unit];
+        vs_next = a.cache.v_scale[unit];
 #pragma unroll
-        for (int n = 0; n < NV; ++n) vc[n] = *(const uint4 *)(vp + (int64_t)(16 * n + q16) * a.cache.block + 16 * g);
+        for (int n = 0; n < NV; ++n) vn[n] = *(const uint4 *)(vp + (16 * n + q16) * a.cache.block + 16 * g);
+        page_next = page_of(step + WAVES);
+    };
+    if (from + wave < to) {
+        page_next = page_of(from + wave);
+        fetch(from + wave);
+    }
+    for (int step = from + wave; step < to; step += WAVES) {
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+            for (int j = 0; j < KL; ++j) kc[kb][j] = kn[kb][j];
+#pragma unroll
+        for (int n = 0; n < NV; ++n) vc[n] = vn[n];
+        const float ks = ks_next, vs = vs_next;
+        const bool page_ok = ok_next;
+        if (step + WAVES < to) fetch(step + WAVES);
 
         float4v sc[NB][4] = {};
 #pragma unroll
@@ -202,6 +226,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_cache_attention(CacheAttentionAr
         }
 
         const float c = fmaxf(a.alpha * kLog2e * ks, 1.17549435e-38f);
+        const int ev = __builtin_amdgcn_readfirstlane(exponent_of(vs));
         if (!begun) eref = ev, begun = true;
         if (ev - eref > kDrift || eref - ev > kDrift) {
             const float f = pow2(eref - ev);
@@ -215,9 +240,9 @@ __global__ __launch_bounds__(WAVES * 64) void k_cache_attention(CacheAttentionAr
         half8 p[NB][2];
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-            float top = fmaxf(fmaxf(sc[nb][0][0], sc[nb][0][1]), fmaxf(sc[nb][0][2], sc[nb][0][3]));
+            float top = most(most(sc[nb][0][0], sc[nb][0][1]), most(sc[nb][0][2], sc[nb][0][3]));
 #pragma unroll
-            for (int kb = 1; kb < 4; ++kb) top = fmaxf(top, fmaxf(fmaxf(sc[nb][kb][0], sc[nb][kb][1]), fmaxf(sc[nb][kb][2], sc[nb][kb][3])));
+            for (int kb = 1; kb < 4; ++kb) top = most(most(top, most(sc[nb][kb][0], sc[nb][kb][1])), most(sc[nb][kb][2], sc[nb][kb][3]));
             top *= c;
             if (__any(top > m[nb] + kSlack)) {
                 const float now = fmaxf(m[nb], max_of_query(top));
@@ -261,40 +286,42 @@ __global__ __launch_bounds__(WAVES * 64) void k_cache_attention(CacheAttentionAr
 #pragma unroll
         for (int n = 0; n < NV; ++n) o[nb][n] *= unit;
     }
-    if constexpr (SHARED) {
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            const int at = wave * R + nb * 16 + q16;
-            if (g == 0) merged_ml[at] = make_float2(m[nb], l[nb]);
+    for (int nb = 0; nb < NB; ++nb) {
+        const int at = wave * R + nb * 16 + q16;
+        if (g == 0) merged_ml[at] = make_float2(m[nb], l[nb]);
 #pragma unroll
-            for (int n = 0; n < NV; ++n) merged[at * (D / 4) + 4 * n + g] = make_float4(o[nb][n][0], o[nb][n][1], o[nb][n][2], o[nb][n][3]);
+        for (int n = 0; n < NV; ++n) merged[at * (D / 4) + 4 * n + g] = make_float4(o[nb][n][0], o[nb][n][1], o[nb][n][2], o[nb][n][3]);
+    }
+    __syncthreads();
+    for (int at = threadIdx.x; at < R * (D / 4); at += WAVES * 64) {
+        const int r = at / (D / 4);
+        if (first + r >= total) continue;
+        float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, merged_ml[w * R + r].x);
+        float4v x = {};
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float2 ml = merged_ml[w * R + r];
+            const float f = ml.x == -INFINITY && ml.y == 0.0f ? 0.0f : exp2f(ml.x - top);  // a NaN among the scores stays one
+            const float4 y = merged[w * R * (D / 4) + at];
+            x += float4v{y.x, y.y, y.z, y.w} * f;
+            sum = fmaf(ml.y, f, sum);
         }
-        __syncthreads();
-        for (int at = threadIdx.x; at < R * (D / 4); at += WAVES * 64) {
-            const int r = at / (D / 4);
-            if (first + r >= total) continue;
-            float top = -INFINITY, sum = 0.0f;
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) top = fmaxf(top, merged_ml[w * R + r].x);
-            float4v x = {};
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) {
-                const float2 ml = merged_ml[w * R + r];
-                const float f = ml.x == -INFINITY && ml.y == 0.0f ? 0.0f : exp2f(ml.x - top);  // a NaN among the scores stays one
-                const float4 y = merged[w * R * (D / 4) + at];
-                x += float4v{y.x, y.y, y.z, y.w} * f;
-                sum = fmaf(ml.y, f, sum);
-            }
-            give<T, D>(a, s, head, group, split, first + r, at % (D / 4) * 4, x, top, sum, at % (D / 4) == 0);
-        }
+        give<T, D>(a, s, head, group, split, first + r, at % (D / 4) * 4, x, top, sum, at % (D / 4) == 0);
     }
 }
 
 // Many rows: each wavefront has NB * 32 of its own, and a workgroup's wavefronts share the keys and values of a step, which
 // reach LDS as 16-bit numbers (each code is widened once for the workgroup, not once for each wavefront), two steps' worth:
 // one is computed with while the next arrives.  Products of 32 x 32: key row 8 i + 4 j + r of a block of 32 is token
-// 16 j + 4 i + r, so a lane again has 16 tokens in a row.  16-byte chunks of a row are swapped by the row's last three bits,
-// which spreads the eight rows that are read at a time over the banks.
+// 16 j + 4 i + r, so a lane again has 16 tokens in a row.  16-byte chunks of a row are swapped by bits of the row's number,
+// which spreads the rows that are read at a time over the banks.
+// (Rows of 16 chunks or more by the row's last four bits, rows of 8 by the three above the last.)
+template <int D>
+__device__ __forceinline__ int key_swap(int row) { return D >= 128 ? row & 15 : row >> 1 & 7; }
+
 template <typename T, int D, int NB, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_cache_attention_rows(CacheAttentionArgs a, int row_tiles)
 {
@@ -355,28 +382,32 @@ __global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_c
     for (int nb = 0; nb < NB; ++nb) m[nb] = -INFINITY, l[nb] = 0.0f;
     int eref = 0;
     bool begun = false;
-    const int per_block = a.cache.block / kCacheTile;
+    const int block_shift = a.cache.block >> 7;  // 64, 128, 256 tokens: 1, 2, 4 steps
 
-    uint4 kc[kUnits], vc[kUnits];  // the next step's codes
-    float ks_next;
-    int ev_next;
-    bool ok_next;
+    // Loads run ahead of what waits for them: a step's codes and scales are asked for one step before, its block two steps
+    // before (the address depends on it).
+    uint4 kc[kUnits], vc[kUnits];
+    float ks_next = 0.0f, vs_next = 0.0f;
+    bool ok_next = false;
+    int page_next;
+    auto page_of = [&](int step) { return a.seq.table[b * a.seq.ldt + (min(step, to - 1) >> block_shift)]; };
     auto fetch = [&](int step) {
-        const int ordinal = step / per_block, sub = step - ordinal * per_block;
-        int page = a.seq.table[b * a.seq.ldt + ordinal];
+        const int sub = step & ((1 << block_shift) - 1);
+        int page = __builtin_amdgcn_readfirstlane(page_next);
         ok_next = page >= 0 && page < a.cache.blocks;
         if (!ok_next) page = 0;
         const int64_t unit = (int64_t)page * H + head;
         const uint8_t *kp = a.cache.k + (unit * a.cache.block + sub * kCacheTile) * D;
         const uint8_t *vp = a.cache.v + unit * D * a.cache.block + sub * kCacheTile;
-        ks_next = a.cache.k_scale[unit];
-        ev_next = exponent_of(a.cache.v_scale[unit]);
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
             const int at = tid + u * NT;
             kc[u] = *(const uint4 *)(kp + 16 * at);
-            vc[u] = *(const uint4 *)(vp + (int64_t)(at >> 2) * a.cache.block + 16 * (at & 3));
+            vc[u] = *(const uint4 *)(vp + (at >> 2) * a.cache.block + 16 * (at & 3));
         }
+        ks_next = a.cache.k_scale[unit];
+        vs_next = a.cache.v_scale[unit];
+        page_next = page_of(step + 1);
     };
     auto stage = [&](int step, int buffer) {
         // a slot behind the sequence holds anything, a NaN too: its weight 0 does not hide that
@@ -384,14 +415,14 @@ __global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_c
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
             const int at = tid + u * NT, token = at / KK, c = 2 * (at % KK);
-            const int row = (token & 32) + 8 * (token >> 2 & 3) + 4 * (token >> 4 & 1) + (token & 3);
+            const int row = (token & 32) + 8 * (token >> 2 & 3) + 4 * (token >> 4 & 1) + (token & 3), k0 = row * (D / 8), swap = key_swap<D>(row);
             union {
                 Frag f;
                 uint4 w;
             } x, y;
             x.f = widen<T>(kc[u].x, kc[u].y), y.f = widen<T>(kc[u].z, kc[u].w);
-            keys[buffer][row * (D / 8) + (c ^ (row & 7))] = x.w;
-            keys[buffer][row * (D / 8) + ((c + 1) ^ (row & 7))] = y.w;
+            keys[buffer][k0 + (c ^ swap)] = x.w;
+            keys[buffer][k0 + ((c + 1) ^ swap)] = y.w;
             const int d = at >> 2, cv = 2 * (at & 3);
             uint4 codes = vc[u];
             if (tail) {
@@ -407,19 +438,19 @@ __global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_c
                 uint4 w;
             } v, z;
             v.f = widen<_Float16>(codes.x, codes.y), z.f = widen<_Float16>(codes.z, codes.w);
-            values[buffer][d * 8 + (cv ^ (d & 7))] = v.w;
-            values[buffer][d * 8 + ((cv + 1) ^ (d & 7))] = z.w;
+            values[buffer][d * 8 + (cv ^ (d >> 1 & 7))] = v.w;
+            values[buffer][d * 8 + ((cv + 1) ^ (d >> 1 & 7))] = z.w;
         }
     };
 
     if (from < to) {
+        page_next = page_of(from);
         fetch(from);
         stage(from, 0);
     }
     for (int step = from; step < to; ++step) {
         const int buffer = (step - from) & 1;
-        const float ks = ks_next;
-        const int ev = ev_next;
+        const float ks = ks_next, vs = vs_next;
         const bool ok = ok_next;
         __syncthreads();
         if (step + 1 < to) fetch(step + 1);
@@ -430,7 +461,7 @@ __global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_c
 #pragma unroll
                 for (int kk = 0; kk < KK; ++kk) {
                     const int row = 32 * kb + q32;
-                    const Frag f = *(const Frag *)&keys[buffer][row * (D / 8) + ((2 * kk + h2) ^ (row & 7))];
+                    const Frag f = *(const Frag *)&keys[buffer][row * (D / 8) + ((2 * kk + h2) ^ key_swap<D>(row))];
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb) sc[nb][kb] = Mma<T>::mma(f, q[nb][kk], sc[nb][kb]);
                 }
@@ -447,6 +478,7 @@ __global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_c
                         }
             }
             const float c = fmaxf(a.alpha * kLog2e * ks, 1.17549435e-38f);
+            const int ev = __builtin_amdgcn_readfirstlane(exponent_of(vs));
             if (!begun) eref = ev, begun = true;
             if (ev - eref > kDrift || eref - ev > kDrift) {
                 const float f = pow2(eref - ev);
@@ -464,7 +496,7 @@ __global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_c
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                    for (int r = 0; r < 16; r += 2) top = fmaxf(top, fmaxf(sc[nb][kb][r], sc[nb][kb][r + 1]));
+                    for (int r = 0; r < 16; r += 2) top = most(top, most(sc[nb][kb][r], sc[nb][kb][r + 1]));
                 top *= c;
                 if (__any(top > m[nb] + kSlack)) {
                     const float now = fmaxf(m[nb], fmaxf(top, __shfl_xor(top, 32)));
@@ -495,7 +527,7 @@ __global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_c
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
                     const int d = 32 * n + q32;
-                    const half8 f = *(const half8 *)&values[buffer][d * 8 + ((4 * (t >> 1) + 2 * h2 + (t & 1)) ^ (d & 7))];
+                    const half8 f = *(const half8 *)&values[buffer][d * 8 + ((4 * (t >> 1) + 2 * h2 + (t & 1)) ^ (d >> 1 & 7))];
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb) o[nb][n] = Mma<_Float16>::mma(f, p[nb][t], o[nb][n]);
                 }
@@ -591,9 +623,9 @@ void launch(const CacheAttentionArgs &a, const Shape &shape, int row_tiles, int6
     if (!shape.shared)
         hipLaunchKernelGGL((k_cache_attention_rows<T, D, 1, kAttWaves>), grid, block, 0, st, a, row_tiles);
     else if (shape.rows == 16)
-        hipLaunchKernelGGL((k_cache_attention<T, D, 1, kAttWaves, true>), grid, block, 0, st, a, row_tiles);
+        hipLaunchKernelGGL((k_cache_attention<T, D, 1, kAttWaves>), grid, block, 0, st, a, row_tiles);
     else
-        hipLaunchKernelGGL((k_cache_attention<T, D, NB, kAttWaves, true>), grid, block, 0, st, a, row_tiles);
+        hipLaunchKernelGGL((k_cache_attention<T, D, NB, kAttWaves>), grid, block, 0, st, a, row_tiles);
     if (a.splits > 1) {
         const int64_t rows = (int64_t)a.seq.batch * a.seq.max_new * a.heads;
         hipLaunchKernelGGL((k_cache_attention_join<T, D>), dim3((unsigned)rows), block, 0, st, a);
