@@ -593,7 +593,7 @@ static int check_cache_call(const bwta_cache *c, int dtype, const int32_t *table
     if (c->block != 64 && c->block != 128 && c->block != 256) return BWTA_ERR_UNSUPPORTED;
     if (c->dim != 64 && c->dim != 128 && c->dim != 256) return BWTA_ERR_UNSUPPORTED;
     if (c->blocks <= 0 || c->kv_heads <= 0 || batch < 0 || M < 0 || max_new < 0 || max_len < 0) return BWTA_ERR_SHAPE;
-    if (c->kv_heads > kMostHeads) return BWTA_ERR_TOO_LARGE;
+    if (c->kv_heads > kMostHeads || max_len > (1 << 30)) return BWTA_ERR_TOO_LARGE;
     if (!cu && (int64_t)batch * max_new > M) return BWTA_ERR_SHAPE;
     if (ldt < ((int64_t)max_len + c->block - 1) / c->block) return BWTA_ERR_SHAPE;
     if (M == 0 || batch == 0 || max_new == 0) {
@@ -672,6 +672,7 @@ int bwta_cache_attention(const bwta_cache *cache, const void *Q, int64_t ldq, vo
     const bwta::SeqArgs s{table, ldt, lens, cu, batch, M, max_new, max_len};
     const int splits = need ? bwta::cache_attention_splits(batch, heads, cache->kv_heads, cache->dim, max_new, max_len) : 1;
     if (bwta::cache_attention_groups(batch, heads, cache->kv_heads, cache->dim, max_new, splits) > kMostGroups) return BWTA_ERR_TOO_LARGE;
+    if ((double)max_new * (heads / cache->kv_heads) > (1u << 31) - 1024.0) return BWTA_ERR_TOO_LARGE;
     return hip_result(bwta::launch_cache_attention({cache_args(cache), s, Q, out, ldq, ldo, lse, heads, alpha, causal != 0, dtype == BWTA_DTYPE_BF16, window,
                                                     (float *)workspace, splits}, (hipStream_t)stream));
 }

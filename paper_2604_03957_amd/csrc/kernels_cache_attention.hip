@@ -72,9 +72,10 @@ __device__ __forceinline__ float sum_of_query(float x)
 
 // Four channels of a row, and once per row its maximum (as a power of two) and sum: the result, or this split's part of it.
 template <typename T, int D>
-__device__ __forceinline__ void give(const CacheAttentionArgs &a, const Seq &s, int head, int group, int split, int64_t row, int channel, float4v x, float m, float l, bool once)
+__device__ __forceinline__ void give(const CacheAttentionArgs &a, const Seq &s, int head, int group, int split, int row, int channel, float4v x, float m, float l, bool once)
 {
-    const int64_t token = s.row + row / group, at = token * a.heads + head * group + row % group;
+    const int t = (unsigned)row / (unsigned)group, h = head * group + (row - t * group);
+    const int64_t token = s.row + t, at = token * a.heads + h;
     if (a.splits > 1) {
         const int64_t all_rows = (int64_t)a.seq.M * a.heads;
         *(float4v *)(a.partial + (split * all_rows + at) * D + channel) = x;
@@ -82,7 +83,7 @@ __device__ __forceinline__ void give(const CacheAttentionArgs &a, const Seq &s, 
         return;
     }
     const float f = l == 0.0f ? 0.0f : 1.0f / l;
-    *(uint2 *)((T *)a.out + token * a.ldo + (head * group + row % group) * D + channel) = make_uint2(Half<T>::pack(x[0] * f, x[1] * f), Half<T>::pack(x[2] * f, x[3] * f));
+    *(uint2 *)((T *)a.out + token * a.ldo + (int64_t)h * D + channel) = make_uint2(Half<T>::pack(x[0] * f, x[1] * f), Half<T>::pack(x[2] * f, x[3] * f));
     if (once && a.lse) a.lse[at] = kLn2 * (m + log2f(l));
 }
 
@@ -104,27 +105,26 @@ __global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_c
     const int bh = i % (a.seq.batch * H), head = bh % H, b = bh / H;
     const int tile_of_rows = row_tiles - 1 - (int)(i / (a.seq.batch * H));  // causal rows at the end see most: first
     const Seq s = sequence(a.seq, b);
-    const int64_t total = (int64_t)s.n * group;
-    const int64_t first = (int64_t)tile_of_rows * R;
+    const int total = min(s.n, a.seq.max_new) * group, first = tile_of_rows * R;  // the host keeps them below 2^31
     if (first >= total) return;
-    const int64_t last = min(first + R, total) - 1;
+    const int last = min(first + R, total) - 1;
 
     // keys that some row sees, and those that every row sees
-    const int t_first = (int)(first / group), t_last = (int)(last / group);
+    const int t_first = (unsigned)first / (unsigned)group, t_last = (unsigned)last / (unsigned)group;
     const int key_end = a.causal ? max(0, min(s.len, s.start + t_last + 1)) : s.len;
     const int key_begin = a.window ? max(0, s.start + t_first - a.window + 1) : 0;
     const int all_end = a.causal ? min(s.len, s.start + t_first + 1) : s.len, all_begin = a.window ? s.start + t_last - a.window + 1 : 0;
     const int step0 = key_begin / kCacheTile, steps = max(0, (key_end + kCacheTile - 1) / kCacheTile - step0);
-    const int from = step0 + (int)((int64_t)steps * split / a.splits), to = step0 + (int)((int64_t)steps * (split + 1) / a.splits);
+    const int from = step0 + (unsigned)(steps * split) / (unsigned)a.splits, to = step0 + (unsigned)(steps * (split + 1)) / (unsigned)a.splits;
 
     // this lane's query of each 16
     int see_lo[NB], see_hi[NB];
     Frag q[NB][2 * KL];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-        const int64_t row = first + nb * 16 + q16;
+        const int row = first + nb * 16 + q16;
         const bool has = row < total;
-        const int t = has ? (int)(row / group) : 0, h = head * group + (has ? (int)(row % group) : 0);
+        const int t = has ? (unsigned)row / (unsigned)group : 0, h = head * group + (has ? row - t * group : 0);
         see_hi[nb] = !has ? -1 : a.causal ? min(s.len - 1, s.start + t) : s.len - 1;
         see_lo[nb] = a.window ? s.start + t - a.window + 1 : 0;
         const T *x = (const T *)a.q + (s.row + t) * a.ldq + (int64_t)h * D;
@@ -313,296 +313,354 @@ __global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_c
     }
 }
 
-// Many rows: each wavefront has NB * 32 of its own, and a workgroup's wavefronts share the keys and values of a step, which
-// reach LDS as 16-bit numbers (each code is widened once for the workgroup, not once for each wavefront), two steps' worth:
-// one is computed with while the next arrives.  Products of 32 x 32: key row 8 i + 4 j + r of a block of 32 is token
-// 16 j + 4 i + r, so a lane again has 16 tokens in a row.  16-byte chunks of a row are swapped by bits of the row's number,
-// which spreads the rows that are read at a time over the banks.
-// (Rows of 16 chunks or more by the row's last four bits, rows of 8 by the three above the last.)
-template <int D>
-__device__ __forceinline__ int key_swap(int row) { return D >= 128 ? row & 15 : row >> 1 & 7; }
+// Where a row's sixteen-byte chunk lies in LDS: rows are one chunk longer than they need be, so that the sixteen rows that are
+// read at a time cover all banks once, and a lane's chunks are constant offsets from one address.
+template <int CHUNKS>
+__device__ __forceinline__ constexpr int padded(int row, int chunk) { return row * (CHUNKS + 1) + chunk; }
 
-template <typename T, int D, int NB, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_cache_attention_rows(CacheAttentionArgs a, int row_tiles)
+// Many rows: each wavefront has 32 of its own, and four wavefronts share the keys and values of a step, which reach LDS as
+// 16-bit numbers (each code is widened once for the four).  Products of 32 x 32: key row 8 i + 4 j + r of a block of 32 is
+// token 16 j + 4 i + r, so a lane again has 16 tokens in a row.
+// A turn computes the scores of the next step beside the weights and the sums of this one: matrix cores and vector ALU have
+// work that does not wait for each other's.  Keys are therefore fetched one step before values.
+// With GROUPS = 2 a workgroup has the rows twice: one four take the even steps, the other the odd ones, and their sums are
+// joined through LDS.
+template <typename T, int D, int GROUPS>
+__global__ __launch_bounds__(GROUPS * 256, D <= 128 ? 2 : 1) void k_cache_attention_rows(CacheAttentionArgs a, int row_tiles)
 {
-    constexpr int R = 32 * NB, kRows = R * WAVES, NT = WAVES * 64, KK = D / 16, DN = D / 32, kUnits = 4 * D / NT;
+    constexpr int WAVES = 4, R = 32, kRows = R * WAVES, NT = WAVES * 64, KK = D / 16, DN = D / 32, kUnits = 4 * D / NT;
     typedef typename Mma<T>::Frag Frag;
-    __shared__ uint4 keys[2][kCacheTile * D / 8], values[2][kCacheTile * D / 8];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), q32 = lane & 31, h2 = lane >> 5;
+    struct Tile {
+        uint4 keys[kCacheTile * (D / 8 + 1)], values[D * (kCacheTile / 8 + 1)];
+    };
+    __shared__ Tile tiles[GROUPS][2];
+    const int side = __builtin_amdgcn_readfirstlane(threadIdx.x / NT), tid = threadIdx.x % NT;
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), q32 = lane & 31, h2 = lane >> 5;
     const int H = a.cache.heads, group = a.heads / H;
 
     unsigned i = blockIdx.x;
     const int split = i % a.splits;
     i /= a.splits;
-    const int bh = i % (a.seq.batch * H), head = bh % H, b = bh / H;
-    const int tile_of_rows = row_tiles - 1 - (int)(i / (a.seq.batch * H));  // causal rows at the end see most: first
+    // Causal rows at the end see most: first.  Workgroups go around the eight XCDs, and inside one around its four shader
+    // engines, in order: consecutive ones have the heads of a sequence, and sequences change places from one round of all of
+    // them to the next, or a long one would always fall to the same engines (half of the time of a ragged batch of four).
+    const int round = (int)(i / (a.seq.batch * H)), bh = i % (a.seq.batch * H), head = bh % H, b = (bh / H + round) % a.seq.batch;
+    const int tile_of_rows = row_tiles - 1 - round;
     const Seq s = sequence(a.seq, b);
-    const int64_t total = (int64_t)s.n * group;
-    const int64_t first = (int64_t)tile_of_rows * kRows;
+    const int total = min(s.n, a.seq.max_new) * group, first = tile_of_rows * kRows;
     if (first >= total) return;
 
-    // keys that some row of rows [lo, lo + count) sees, and those that every one sees
-    struct Span {
-        int begin, end, all_begin, all_end;
-    };
-    auto span = [&](int64_t lo, int count) {
-        const int64_t hi = min(lo + count, total) - 1;
-        const int t0 = (int)(lo / group), t1 = (int)(hi / group);
-        Span r;
-        r.end = hi < lo ? 0 : a.causal ? max(0, min(s.len, s.start + t1 + 1)) : s.len;
-        r.begin = a.window ? max(0, s.start + t0 - a.window + 1) : 0;
-        r.all_end = a.causal ? min(s.len, s.start + t0 + 1) : s.len;
-        r.all_begin = a.window ? s.start + t1 - a.window + 1 : 0;
-        return r;
-    };
-    const Span whole = span(first, kRows), mine = span(first + wave * R, R);
-    const int step0 = whole.begin / kCacheTile, steps = max(0, (whole.end + kCacheTile - 1) / kCacheTile - step0);
-    const int from = step0 + (int)((int64_t)steps * split / a.splits), to = step0 + (int)((int64_t)steps * (split + 1) / a.splits);
+    // keys that some row sees, and those that every row of this wavefront sees
+    const int my_first = min(first + wave * R, total - 1), my_last = min(my_first + R, total) - 1, last = min(first + kRows, total) - 1;
+    const int t_first = (unsigned)first / (unsigned)group, t_last = (unsigned)last / (unsigned)group;
+    const int key_end = a.causal ? max(0, min(s.len, s.start + t_last + 1)) : s.len;
+    const int key_begin = a.window ? max(0, s.start + t_first - a.window + 1) : 0;
+    const int all_end = a.causal ? min(s.len, s.start + (int)((unsigned)my_first / (unsigned)group) + 1) : s.len;
+    const int all_begin = a.window ? s.start + (int)((unsigned)my_last / (unsigned)group) - a.window + 1 : 0;
+    const int step0 = key_begin / kCacheTile, steps = max(0, (key_end + kCacheTile - 1) / kCacheTile - step0);
+    const int from = step0 + (unsigned)(steps * split) / (unsigned)a.splits, to = step0 + (unsigned)(steps * (split + 1)) / (unsigned)a.splits;
 
-    int see_lo[NB], see_hi[NB];
-    Frag q[NB][KK];
+    // this lane's query
+    const int row = first + wave * R + q32;
+    const bool has = row < total;
+    const int token = has ? (unsigned)row / (unsigned)group : 0;
+    const int see_hi = !has ? -1 : a.causal ? min(s.len - 1, s.start + token) : s.len - 1, see_lo = a.window ? s.start + token - a.window + 1 : 0;
+    Frag q[KK];
+    const T *query = (const T *)a.q + (s.row + token) * a.ldq + (int64_t)(head * group + (has ? row - token * group : 0)) * D + 8 * h2;
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-        const int64_t row = first + wave * R + nb * 32 + q32;
-        const bool has = row < total;
-        const int t = has ? (int)(row / group) : 0, h = head * group + (has ? (int)(row % group) : 0);
-        see_hi[nb] = !has ? -1 : a.causal ? min(s.len - 1, s.start + t) : s.len - 1;
-        see_lo[nb] = a.window ? s.start + t - a.window + 1 : 0;
-        const T *x = (const T *)a.q + (s.row + t) * a.ldq + (int64_t)h * D;
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk) {
-            if (has) q[nb][kk] = *(const Frag *)(x + 16 * kk + 8 * h2);
-            else q[nb][kk] = Frag{};
-        }
+    for (int kk = 0; kk < KK; ++kk) {
+        if (has) q[kk] = *(const Frag *)(query + 16 * kk);
+        else q[kk] = Frag{};
     }
 
-    float16v o[NB][DN] = {};
-    float m[NB], l[NB];
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) m[nb] = -INFINITY, l[nb] = 0.0f;
+    float16v o[DN] = {};
+    float m = -INFINITY, l = 0.0f, top = -INFINITY;
     int eref = 0;
-    bool begun = false;
     const int block_shift = a.cache.block >> 7;  // 64, 128, 256 tokens: 1, 2, 4 steps
 
-    // Loads run ahead of what waits for them: a step's codes and scales are asked for one step before, its block two steps
-    // before (the address depends on it).
+    // Loads run ahead of what waits for them.  Steps behind the last are the last again, so that nothing branches on them.
     uint4 kc[kUnits], vc[kUnits];
-    float ks_next = 0.0f, vs_next = 0.0f;
-    bool ok_next = false;
-    int page_next;
+    struct Step {
+        int64_t unit;
+        int step;
+        float ks, vs;
+        bool ok, none;
+    };
+    int page_ahead;
     auto page_of = [&](int step) { return a.seq.table[b * a.seq.ldt + (min(step, to - 1) >> block_shift)]; };
-    auto fetch = [&](int step) {
-        const int sub = step & ((1 << block_shift) - 1);
-        int page = __builtin_amdgcn_readfirstlane(page_next);
-        ok_next = page >= 0 && page < a.cache.blocks;
-        if (!ok_next) page = 0;
-        const int64_t unit = (int64_t)page * H + head;
-        const uint8_t *kp = a.cache.k + (unit * a.cache.block + sub * kCacheTile) * D;
-        const uint8_t *vp = a.cache.v + unit * D * a.cache.block + sub * kCacheTile;
+    auto next_step = [&](int step) {  // also asks for the block of the step behind it
+        Step r;
+        r.step = min(step, to - 1);
+        r.none = step >= to;
+        const int page = __builtin_amdgcn_readfirstlane(page_ahead);
+        r.ok = page >= 0 && page < a.cache.blocks;
+        r.unit = (int64_t)(r.ok ? page : 0) * H + head;
+        r.ks = a.cache.k_scale[r.unit];
+        r.vs = a.cache.v_scale[r.unit];
+        page_ahead = page_of(step + GROUPS);
+        return r;
+    };
+    auto fetch_keys = [&](const Step &n) {
+        const uint8_t *kp = a.cache.k + (n.unit * a.cache.block + (n.step & ((1 << block_shift) - 1)) * kCacheTile) * D;
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) kc[u] = *(const uint4 *)(kp + 16 * (tid + u * NT));
+    };
+    auto fetch_values = [&](const Step &n) {
+        const uint8_t *vp = a.cache.v + n.unit * D * a.cache.block + (n.step & ((1 << block_shift) - 1)) * kCacheTile;
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
             const int at = tid + u * NT;
-            kc[u] = *(const uint4 *)(kp + 16 * at);
             vc[u] = *(const uint4 *)(vp + (at >> 2) * a.cache.block + 16 * (at & 3));
         }
-        ks_next = a.cache.k_scale[unit];
-        vs_next = a.cache.v_scale[unit];
-        page_next = page_of(step + 1);
     };
-    auto stage = [&](int step, int buffer) {
-        // a slot behind the sequence holds anything, a NaN too: its weight 0 does not hide that
-        const bool tail = !ok_next || (step + 1) * kCacheTile > s.len;
+    auto stage_keys = [&](int buffer) {
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
             const int at = tid + u * NT, token = at / KK, c = 2 * (at % KK);
-            const int row = (token & 32) + 8 * (token >> 2 & 3) + 4 * (token >> 4 & 1) + (token & 3), k0 = row * (D / 8), swap = key_swap<D>(row);
-            union {
-                Frag f;
-                uint4 w;
-            } x, y;
-            x.f = widen<T>(kc[u].x, kc[u].y), y.f = widen<T>(kc[u].z, kc[u].w);
-            keys[buffer][k0 + (c ^ swap)] = x.w;
-            keys[buffer][k0 + ((c + 1) ^ swap)] = y.w;
-            const int d = at >> 2, cv = 2 * (at & 3);
-            uint4 codes = vc[u];
-            if (tail) {
-                const int valid = ok_next ? s.len - step * kCacheTile - 16 * (at & 3) : 0;
+            const int row = (token & 32) + 8 * (token >> 2 & 3) + 4 * (token >> 4 & 1) + (token & 3);
+            *(Frag *)&tiles[side][buffer].keys[padded<D / 8>(row, c)] = widen<T>(kc[u].x, kc[u].y);
+            *(Frag *)&tiles[side][buffer].keys[padded<D / 8>(row, c + 1)] = widen<T>(kc[u].z, kc[u].w);
+        }
+    };
+    auto stage_values = [&](const Step &n, int buffer) {
+        // a slot behind the sequence holds anything, a NaN too: its weight 0 does not hide that
+        if (!n.ok || (n.step + 1) * kCacheTile > s.len) {
+#pragma unroll
+            for (int u = 0; u < kUnits; ++u) {
+                const int valid = n.ok ? s.len - n.step * kCacheTile - 16 * ((tid + u * NT) & 3) : 0;
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     const int bytes = min(max(valid - 4 * w, 0), 4);
-                    (&codes.x)[w] &= bytes == 4 ? 0xffffffffu : (1u << (8 * bytes)) - 1;
+                    (&vc[u].x)[w] &= bytes == 4 ? 0xffffffffu : (1u << (8 * bytes)) - 1;
                 }
             }
-            union {
-                half8 f;
-                uint4 w;
-            } v, z;
-            v.f = widen<_Float16>(codes.x, codes.y), z.f = widen<_Float16>(codes.z, codes.w);
-            values[buffer][d * 8 + (cv ^ (d >> 1 & 7))] = v.w;
-            values[buffer][d * 8 + ((cv + 1) ^ (d >> 1 & 7))] = z.w;
+        }
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const int at = tid + u * NT, d = at >> 2, c = 2 * (at & 3);
+            *(half8 *)&tiles[side][buffer].values[padded<8>(d, c)] = widen<_Float16>(vc[u].x, vc[u].y);
+            *(half8 *)&tiles[side][buffer].values[padded<8>(d, c + 1)] = widen<_Float16>(vc[u].z, vc[u].w);
         }
     };
 
-    if (from < to) {
-        page_next = page_of(from);
-        fetch(from);
-        stage(from, 0);
-    }
-    for (int step = from; step < to; ++step) {
-        const int buffer = (step - from) & 1;
-        const float ks = ks_next, vs = vs_next;
-        const bool ok = ok_next;
-        __syncthreads();
-        if (step + 1 < to) fetch(step + 1);
-        if (ok && step * kCacheTile < mine.end && (step + 1) * kCacheTile > mine.begin) {  // else no row of this wavefront sees any of these keys
-            float16v sc[NB][2] = {};
+    float16v now[2], ahead[2];  // scores of this step and of the next
+    auto hide = [&](const Step &n) {  // keys that a row does not see
+        if (!n.ok || n.none || (n.step + 1) * kCacheTile > all_end || n.step * kCacheTile < all_begin) {
+            const int key0 = n.step * kCacheTile + 16 * h2, hi = n.ok && !n.none ? see_hi : -1;
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                for (int kk = 0; kk < KK; ++kk) {
-                    const int row = 32 * kb + q32;
-                    const Frag f = *(const Frag *)&keys[buffer][row * (D / 8) + ((2 * kk + h2) ^ key_swap<D>(row))];
-#pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) sc[nb][kb] = Mma<T>::mma(f, q[nb][kk], sc[nb][kb]);
+                for (int r = 0; r < 16; ++r) {
+                    const int key = key0 + 32 * kb + r;
+                    ahead[kb][r] = ((key > hi) | (key < see_lo)) ? -INFINITY : ahead[kb][r];
                 }
-            if ((step + 1) * kCacheTile > mine.all_end || step * kCacheTile < mine.all_begin) {
-                const int key0 = step * kCacheTile + 16 * h2;
+        }
+    };
+    auto largest = [&] {
+        float x = -INFINITY;
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb)
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                    for (int kb = 0; kb < 2; ++kb)
+            for (int r = 0; r < 16; r += 2) x = most(x, most(ahead[kb][r], ahead[kb][r + 1]));
+        return x;
+    };
+    auto score = [&](int buffer, int kb, int kk) {
+        const Frag f = *(const Frag *)&tiles[side][buffer].keys[padded<D / 8>(32 * kb + q32, 2 * kk + h2)];
+        ahead[kb] = Mma<T>::mma(f, q[kk], kk == 0 ? float16v{} : ahead[kb]);
+    };
+
+    if (from < to) {
+        page_ahead = page_of(from + side);
+        Step s0 = next_step(from + side);
+        fetch_keys(s0);
+        fetch_values(s0);
+        stage_keys(0);
+        stage_values(s0, 0);
+        Step s1 = next_step(from + side + GROUPS);
+        fetch_keys(s1);
+        stage_keys(1);
+        __syncthreads();
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            const int key = key0 + 32 * kb + r;
-                            sc[nb][kb][r] = ((key > see_hi[nb]) | (key < see_lo[nb])) ? -INFINITY : sc[nb][kb][r];
-                        }
-            }
-            const float c = fmaxf(a.alpha * kLog2e * ks, 1.17549435e-38f);
-            const int ev = __builtin_amdgcn_readfirstlane(exponent_of(vs));
-            if (!begun) eref = ev, begun = true;
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) score(0, kb, kk);
+        hide(s0);
+        top = largest();
+        eref = __builtin_amdgcn_readfirstlane(exponent_of(s0.vs));
+
+        for (int turn = from; turn < to; turn += GROUPS) {
+            const int buffer = (turn - from) / GROUPS & 1, step = turn + side;
+            __syncthreads();  // keys of the next step and values of this one are there, and nobody reads what is written below
+            const Step s2 = next_step(step + 2 * GROUPS);
+            fetch_keys(s2);
+            fetch_values(s1);
+
+            const float c = fmaxf(a.alpha * kLog2e * s0.ks, 1.17549435e-38f);
+            const int ev = __builtin_amdgcn_readfirstlane(exponent_of(s0.vs));
             if (ev - eref > kDrift || eref - ev > kDrift) {
                 const float f = pow2(eref - ev);
                 eref = ev;
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-                    for (int n = 0; n < DN; ++n) o[nb][n] *= f;
+                for (int n = 0; n < DN; ++n) o[n] *= f;
             }
             const float drift = (float)(ev - eref), undrift = pow2(eref - ev);
-            half8 p[NB][4];
+            top *= c;
+            if (__any(top > m + kSlack)) {
+                const float up = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)));
+                const float f = m == -INFINITY ? 0.0f : exp2f(m - up);
+                m = up;
+                l *= f;
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                float top = -INFINITY;
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                    for (int r = 0; r < 16; r += 2) top = most(top, most(sc[nb][kb][r], sc[nb][kb][r + 1]));
-                top *= c;
-                if (__any(top > m[nb] + kSlack)) {
-                    const float now = fmaxf(m[nb], fmaxf(top, __shfl_xor(top, 32)));
-                    const float f = m[nb] == -INFINITY ? 0.0f : exp2f(m[nb] - now);
-                    m[nb] = now;
-                    l[nb] *= f;
-#pragma unroll
-                    for (int n = 0; n < DN; ++n) o[nb][n] *= f;
-                }
-                const float base = (m[nb] == -INFINITY ? 0.0f : m[nb]) - drift;
-                float sum[4] = {};
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                    for (int hf = 0; hf < 2; ++hf) {
-                        float w[8];
-#pragma unroll
-                        for (int r = 0; r < 8; ++r) {
-                            w[r] = __builtin_amdgcn_exp2f(fmaf(sc[nb][kb][8 * hf + r], c, -base));
-                            sum[r & 3] += w[r];
-                        }
-                        p[nb][2 * kb + hf] = half8{(_Float16)w[0], (_Float16)w[1], (_Float16)w[2], (_Float16)w[3], (_Float16)w[4], (_Float16)w[5], (_Float16)w[6], (_Float16)w[7]};
-                    }
-                l[nb] = fmaf((sum[0] + sum[1]) + (sum[2] + sum[3]), undrift, l[nb]);
+                for (int n = 0; n < DN; ++n) o[n] *= f;
             }
+            const float base = (m == -INFINITY ? 0.0f : m) - drift;
+            now[0] = ahead[0], now[1] = ahead[1];
+
+            float sum[4] = {};
+            half8 p[4];
+            auto weigh = [&](int t) {
+                float w[8];
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    w[r] = __builtin_amdgcn_exp2f(fmaf(now[t >> 1][8 * (t & 1) + r], c, -base));
+                    sum[r & 3] += w[r];
+                }
+                p[t] = half8{(_Float16)w[0], (_Float16)w[1], (_Float16)w[2], (_Float16)w[3], (_Float16)w[4], (_Float16)w[5], (_Float16)w[6], (_Float16)w[7]};
+            };
+            auto gather = [&](int n, int t) {
+                const half8 f = *(const half8 *)&tiles[side][buffer].values[padded<8>(32 * n + q32, 4 * (t >> 1) + 2 * h2 + (t & 1))];
+                o[n] = Mma<_Float16>::mma(f, p[t], o[n]);
+            };
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) {
+                score(buffer ^ 1, 0, kk);
+                score(buffer ^ 1, 1, kk);
+                if (kk % (KK / 4) == 0) weigh(kk / (KK / 4));
+            }
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int n = 0; n < DN; ++n) gather(n, t);
+            l = fmaf((sum[0] + sum[1]) + (sum[2] + sum[3]), undrift, l);
+            hide(s1);
+            top = largest();
+            stage_keys(buffer);
+            stage_values(s1, buffer ^ 1);
+            s0 = s1, s1 = s2;
+        }
+    }
+
+    // o[n][r]: query q32, channel 32 n + 8 (r / 4) + 4 h2 + r % 4, in units of 2^eref
+    const float unit = pow2(eref);
+    float4v x[DN][4];
+    l += __shfl_xor(l, 32);
+#pragma unroll
+    for (int n = 0; n < DN; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[n][r] = float4v{o[n][4 * r], o[n][4 * r + 1], o[n][4 * r + 2], o[n][4 * r + 3]} * unit;
+    if constexpr (GROUPS == 2) {
+        constexpr int kSums = DN * 4 * NT;
+        static_assert(sizeof(tiles) >= kSums * sizeof(float4v) + NT * sizeof(float2), "the sums go where keys and values were");
+        float4v *const sums = (float4v *)&tiles[0][0];
+        float2 *const ml = (float2 *)(sums + kSums);
+        __syncthreads();
+        if (side) {
+            ml[tid] = make_float2(m, l);
 #pragma unroll
             for (int n = 0; n < DN; ++n)
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const int d = 32 * n + q32;
-                    const half8 f = *(const half8 *)&values[buffer][d * 8 + ((4 * (t >> 1) + 2 * h2 + (t & 1)) ^ (d >> 1 & 7))];
-#pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) o[nb][n] = Mma<_Float16>::mma(f, p[nb][t], o[nb][n]);
-                }
+                for (int r = 0; r < 4; ++r) sums[(n * 4 + r) * NT + tid] = x[n][r];
         }
-        if (step + 1 < to) stage(step + 1, buffer ^ 1);
-    }
-
-    // o[nb][n][r]: query q32 of the nb-th 32, channel 32 n + 8 (r / 4) + 4 h2 + r % 4, in units of 2^eref
-    const float unit = pow2(eref);
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-        const float sum = l[nb] + __shfl_xor(l[nb], 32);
-        const int64_t row = first + wave * R + nb * 32 + q32;
-        if (row >= total) continue;
+        __syncthreads();
+        if (side) return;
+        const float2 other = ml[tid];
+        top = fmaxf(m, other.x);
+        const float f = m == -INFINITY && l == 0.0f ? 0.0f : exp2f(m - top);  // a NaN among the scores stays one
+        const float g = other.x == -INFINITY && other.y == 0.0f ? 0.0f : exp2f(other.x - top);
+        m = top;
+        l = l * f + other.y * g;
 #pragma unroll
         for (int n = 0; n < DN; ++n)
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                give<T, D>(a, s, head, group, split, row, 32 * n + 8 * r + 4 * h2, float4v{o[nb][n][4 * r], o[nb][n][4 * r + 1], o[nb][n][4 * r + 2], o[nb][n][4 * r + 3]} * unit,
-                           m[nb], sum, n == 0 && r == 0 && h2 == 0);
+            for (int r = 0; r < 4; ++r) x[n][r] = x[n][r] * f + sums[(n * 4 + r) * NT + tid] * g;
     }
+    if (!has) return;
+#pragma unroll
+    for (int n = 0; n < DN; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) give<T, D>(a, s, head, group, split, row, 32 * n + 8 * r + 4 * h2, x[n][r], m, l, n == 0 && r == 0 && h2 == 0);
 }
 
-// The parts of one row: a workgroup per row, some threads for each four channels.
-constexpr int kMostSplits = 128;
-template <typename T, int D>
+// The parts of a row: D / 4 threads have four channels each, ALONE of them a row for themselves (few parts, many rows), or
+// all of a workgroup's threads one row, each D / 4 some of its parts.
+constexpr int kMostSplits = 128, kFewSplits = 8;
+template <typename T, int D, bool ALONE>
 __global__ __launch_bounds__(256) void k_cache_attention_join(CacheAttentionArgs a)
 {
-    constexpr int C = D / 4, kSide = 256 / C;  // parts side by side
-    __shared__ float weight[kMostSplits], total[2];
-    __shared__ float4v side[kSide][C];
-    const int tid = threadIdx.x, h = (int)(blockIdx.x % a.heads);
-    const unsigned bt = blockIdx.x / a.heads;
-    const int b = (int)(bt / a.seq.max_new), t = (int)(bt % a.seq.max_new);
+    constexpr int C = D / 4, kSide = 256 / C;
+    __shared__ float weight[ALONE ? 1 : kMostSplits], total[2];
+    __shared__ float4v side[ALONE ? 1 : kSide][C];
+    const int tid = threadIdx.x, c = tid % C, nth = tid / C;
+    const unsigned item = ALONE ? blockIdx.x * kSide + nth : blockIdx.x, bt = item / a.heads;
+    const int h = item % a.heads, b = bt / a.seq.max_new, t = bt % a.seq.max_new;
+    if (ALONE && b >= a.seq.batch) return;
     const Seq s = sequence(a.seq, b);
     if (t >= s.n) return;
     const int64_t all_rows = (int64_t)a.seq.M * a.heads, row = (int64_t)(s.row + t) * a.heads + h;
-    if (tid < 64) {
-        const float2 *ml = (const float2 *)(a.partial + a.splits * all_rows * D) + row;
-        float2 p[kMostSplits / 64];
-        float top = -INFINITY, sum = 0.0f;
-#pragma unroll
-        for (int j = 0; j < kMostSplits / 64; ++j) {
-            p[j] = tid + 64 * j < a.splits ? ml[(tid + 64 * j) * all_rows] : make_float2(-INFINITY, 0.0f);
-            top = fmaxf(top, p[j].x);
-        }
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-#pragma unroll
-        for (int j = 0; j < kMostSplits / 64; ++j) {
-            const float f = p[j].x == -INFINITY && p[j].y == 0.0f ? 0.0f : exp2f(p[j].x - top);
-            weight[tid + 64 * j] = f;
-            sum = fmaf(f, p[j].y, sum);
-        }
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-        if (tid == 0) total[0] = top, total[1] = sum;
-    }
-    __syncthreads();
-    const int c = tid % C, first = tid / C;
+    const float2 *ml = (const float2 *)(a.partial + a.splits * all_rows * D) + row;
     const float *o = a.partial + row * D + 4 * c;
     float4v x = {};
-#pragma unroll 4
-    for (int k = first; k < a.splits; k += kSide) x += *(const float4v *)(o + k * all_rows * D) * weight[k];
-    side[first][c] = x;
-    __syncthreads();
-    if (first) return;
+    float top = -INFINITY, sum = 0.0f;
+    if constexpr (ALONE) {
+        float2 p[kFewSplits];
 #pragma unroll
-    for (int k = 1; k < kSide; ++k) x += side[k][c];
-    const float sum = total[1], f = sum == 0.0f ? 0.0f : 1.0f / sum;
+        for (int k = 0; k < kFewSplits; ++k) {
+            p[k] = k < a.splits ? ml[k * all_rows] : make_float2(-INFINITY, 0.0f);
+            top = fmaxf(top, p[k].x);
+        }
+#pragma unroll
+        for (int k = 0; k < kFewSplits; ++k) {
+            if (k >= a.splits) break;
+            const float f = p[k].x == -INFINITY && p[k].y == 0.0f ? 0.0f : exp2f(p[k].x - top);  // a NaN among the scores stays one
+            sum = fmaf(f, p[k].y, sum);
+            x += *(const float4v *)(o + k * all_rows * D) * f;
+        }
+    } else {
+        if (tid < 64) {
+            float2 p[kMostSplits / 64];
+#pragma unroll
+            for (int j = 0; j < kMostSplits / 64; ++j) {
+                p[j] = tid + 64 * j < a.splits ? ml[(tid + 64 * j) * all_rows] : make_float2(-INFINITY, 0.0f);
+                top = fmaxf(top, p[j].x);
+            }
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+#pragma unroll
+            for (int j = 0; j < kMostSplits / 64; ++j) {
+                const float f = p[j].x == -INFINITY && p[j].y == 0.0f ? 0.0f : exp2f(p[j].x - top);
+                weight[tid + 64 * j] = f;
+                sum = fmaf(f, p[j].y, sum);
+            }
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+            if (tid == 0) total[0] = top, total[1] = sum;
+        }
+        __syncthreads();
+#pragma unroll 4
+        for (int k = nth; k < a.splits; k += kSide) x += *(const float4v *)(o + k * all_rows * D) * weight[k];
+        side[nth][c] = x;
+        __syncthreads();
+        if (nth) return;
+#pragma unroll
+        for (int k = 1; k < kSide; ++k) x += side[k][c];
+        top = total[0], sum = total[1];
+    }
+    const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
     *(uint2 *)((T *)a.out + (s.row + t) * a.ldo + (int64_t)h * D + 4 * c) = make_uint2(Half<T>::pack(x[0] * f, x[1] * f), Half<T>::pack(x[2] * f, x[3] * f));
-    if (c == 0 && a.lse) a.lse[row] = kLn2 * (total[0] + log2f(sum));
+    if (c == 0 && a.lse) a.lse[row] = kLn2 * (top + log2f(sum));
 }
 
-// Rows a workgroup takes: up to 16 or 32 shared by four wavefronts, else 32 for each of four.
+// Rows a workgroup takes: up to 16 or 32 that its four wavefronts share, else 32 for each of four (or of twice four).
 struct Shape {
     int rows;
     bool shared;
@@ -620,15 +678,27 @@ void launch(const CacheAttentionArgs &a, const Shape &shape, int row_tiles, int6
 {
     constexpr int NB = D < 256 ? 2 : 1;
     const dim3 grid((unsigned)groups), block(kAttWaves * 64);
-    if (!shape.shared)
-        hipLaunchKernelGGL((k_cache_attention_rows<T, D, 1, kAttWaves>), grid, block, 0, st, a, row_tiles);
-    else if (shape.rows == 16)
+    if (!shape.shared) {
+        // Two workgroups' worth of wavefronts on the same rows halve the way of the rows that see most, which is what few
+        // workgroups take their time for; many balance by themselves, unless long sequences of a batch differ.  us, one / two,
+        // heads of 128: a causal prompt of 2048 with 32 heads 58 / 55, two of them 95 / 109; 128 rows over 256 keys, 32 times,
+        // 40 / 56; chunks of up to 1024 tokens over 5163 to 16024 keys, four times, 641 / 610.
+        constexpr int kMost = D <= 128 ? 2 : 1;
+        const bool differ = a.seq.batch > 1 && a.seq.max_len >= 8192;
+        if (kMost == 2 && a.seq.max_len >= 1024 && groups <= (differ ? 1024 : 512))
+            hipLaunchKernelGGL((k_cache_attention_rows<T, D, kMost>), grid, dim3(kMost * 256), 0, st, a, row_tiles);
+        else
+            hipLaunchKernelGGL((k_cache_attention_rows<T, D, 1>), grid, block, 0, st, a, row_tiles);
+    } else if (shape.rows == 16)
         hipLaunchKernelGGL((k_cache_attention<T, D, 1, kAttWaves>), grid, block, 0, st, a, row_tiles);
     else
         hipLaunchKernelGGL((k_cache_attention<T, D, NB, kAttWaves>), grid, block, 0, st, a, row_tiles);
     if (a.splits > 1) {
-        const int64_t rows = (int64_t)a.seq.batch * a.seq.max_new * a.heads;
-        hipLaunchKernelGGL((k_cache_attention_join<T, D>), dim3((unsigned)rows), block, 0, st, a);
+        const int64_t rows = (int64_t)a.seq.batch * a.seq.max_new * a.heads, alone = 256 / (D / 4);
+        if (a.splits <= kFewSplits)
+            hipLaunchKernelGGL((k_cache_attention_join<T, D, true>), dim3((unsigned)((rows + alone - 1) / alone)), block, 0, st, a);
+        else
+            hipLaunchKernelGGL((k_cache_attention_join<T, D, false>), dim3((unsigned)rows), block, 0, st, a);
     }
 }
 
@@ -655,9 +725,9 @@ int cache_attention_splits(int batch, int heads, int kv_heads, int dim, int max_
     const Shape shape = shape_of(rows, dim);
     const double groups = cache_attention_groups(batch, heads, kv_heads, dim, max_new, 1);
     const int64_t steps = ((int64_t)max_len + kCacheTile - 1) / kCacheTile;
-    // four workgroups for every compute unit, as long as each of their wavefronts still has a few steps
-    if (!shape.shared && groups >= 256) return 1;
-    const int64_t want = groups >= 1024 ? 1 : (int64_t)((1024 + groups - 1) / groups), most = steps / (shape.shared ? kAttWaves : 4);
+    // Four workgroups for every compute unit, as long as each of their wavefronts still has a few steps; of many rows, whose
+    // parts are large, one, with 16 steps at least.
+    const int64_t full = shape.shared ? 1024 : 256, want = groups >= full ? 1 : (int64_t)((full + groups - 1) / groups), most = steps / (shape.shared ? kAttWaves : 16);
     const int64_t s = want < most ? want : most;
     return (int)(s < 1 ? 1 : s > kMostSplits ? kMostSplits : s);
 }
