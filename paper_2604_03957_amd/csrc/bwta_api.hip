@@ -647,8 +647,7 @@ int bwta_cache_read(const bwta_cache *cache, void *K, int64_t ldk, void *V, int6
 size_t bwta_cache_attention_workspace_bytes(int M, int heads, int kv_heads, int dim, int batch, int max_new, int max_len)
 {
     if (M <= 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || heads > kMostHeads || dim <= 0 || dim > 256 || batch <= 0 || max_new <= 0 || max_len <= 0) return 0;
-    const int splits = bwta::cache_attention_splits(batch, heads, kv_heads, dim, max_new, max_len);
-    return splits > 1 ? round_up((size_t)splits * M * heads * (dim + 2) * sizeof(float), 256) : 0;
+    return round_up(bwta::cache_attention_plan(M, heads, kv_heads, dim, batch, max_new, max_len).workspace, 256);
 }
 
 int bwta_cache_attention(const bwta_cache *cache, const void *Q, int64_t ldq, void *out, int64_t ldo, int dtype, float *lse,
@@ -670,11 +669,11 @@ int bwta_cache_attention(const bwta_cache *cache, const void *Q, int64_t ldq, vo
     if (need && (!workspace || workspace_bytes < need)) return BWTA_ERR_WORKSPACE;
     if (need && !aligned(workspace, 256)) return BWTA_ERR_ALIGN;
     const bwta::SeqArgs s{table, ldt, lens, cu, batch, M, max_new, max_len};
-    const int splits = need ? bwta::cache_attention_splits(batch, heads, cache->kv_heads, cache->dim, max_new, max_len) : 1;
-    if (bwta::cache_attention_groups(batch, heads, cache->kv_heads, cache->dim, max_new, splits) > kMostGroups) return BWTA_ERR_TOO_LARGE;
-    if ((double)max_new * (heads / cache->kv_heads) > (1u << 31) - 1024.0) return BWTA_ERR_TOO_LARGE;
+    const bwta::AttentionPlan plan = bwta::cache_attention_plan(M, heads, cache->kv_heads, cache->dim, batch, max_new, max_len);
+    if (plan.groups > kMostGroups || (double)max_new * (heads / cache->kv_heads) > (1u << 31) - 1024.0 || (plan.workspace && (double)batch * max_new * heads > kMostGroups))
+        return BWTA_ERR_TOO_LARGE;
     return hip_result(bwta::launch_cache_attention({cache_args(cache), s, Q, out, ldq, ldo, lse, heads, alpha, causal != 0, dtype == BWTA_DTYPE_BF16, window,
-                                                    (float *)workspace, splits}, (hipStream_t)stream));
+                                                    (float *)workspace, 0, 1, -1, 0}, plan, (hipStream_t)stream));
 }
 
 const char *bwta_strerror(int code)

@@ -33,6 +33,7 @@ struct Seq {
 __device__ __forceinline__ Seq sequence(const SeqArgs &a, int b)
 {
     Seq s;
+    const int len = a.lens[b];
     int lo, hi;
     if (a.cu) {
         lo = min(max(a.cu[b], 0), a.M);
@@ -43,7 +44,7 @@ __device__ __forceinline__ Seq sequence(const SeqArgs &a, int b)
     }
     s.row = lo;
     s.n = hi - lo;
-    s.len = min(max(a.lens[b], 0), a.max_len);
+    s.len = min(max(len, 0), a.max_len);
     s.start = s.len - s.n;
     return s;
 }
@@ -148,11 +149,21 @@ struct CacheAttentionArgs {
     float alpha;
     bool causal, bf16;
     int window;
-    float *partial;  // [splits][M * heads][dim] sums, then [splits][M * heads][2] maximum and sum of weights
-    int splits;
+    // Parts of rows that are joined afterwards: [part_rows][dim] sums, then [part_rows][2] maximum and sum of weights.  Many
+    // rows: [splits][M * heads].  Few (share_rows of them a workgroup): [batch * key heads][splits][share_rows], or where
+    // 2^share_log2 workgroups share all steps (-1: they do not) [workgroups][2][share_rows], and behind the parts how many
+    // steps lie before each sequence.
+    float *partial;
+    int64_t part_rows;
+    int splits, share_log2, share_rows;
 };
-int cache_attention_splits(int batch, int heads, int kv_heads, int dim, int max_new, int max_len);
-double cache_attention_groups(int batch, int heads, int kv_heads, int dim, int max_new, int splits);
-hipError_t launch_cache_attention(const CacheAttentionArgs &a, hipStream_t st);
+struct AttentionPlan {
+    int rows, row_tiles, splits, share_log2;
+    double groups;  // workgroups
+    int64_t part_rows;
+    size_t workspace;  // bytes
+};
+AttentionPlan cache_attention_plan(int M, int heads, int kv_heads, int dim, int batch, int max_new, int max_len);
+hipError_t launch_cache_attention(CacheAttentionArgs a, const AttentionPlan &plan, hipStream_t st);
 
 }  // namespace bwta

@@ -23,6 +23,16 @@ typedef __bf16 bf2v __attribute__((ext_vector_type(2)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 
+typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
+
+// what one wavefront reads once: past the caches' replacement order (a batch of 32 sequences of 4096 tokens, 32 key heads: 5.1
+// TB/s without, 6.2 with)
+__device__ __forceinline__ uint4 load_once(const uint8_t *p)
+{
+    const uint4v x = __builtin_nontemporal_load((const uint4v *)p);
+    return make_uint4(x.x, x.y, x.z, x.w);
+}
+
 template <typename T> struct Mma;
 template <> struct Mma<_Float16> {
     typedef half8 Frag;
@@ -70,27 +80,48 @@ __device__ __forceinline__ float sum_of_query(float x)
     return x + __shfl_xor(x, 32);
 }
 
-// Four channels of a row, and once per row its maximum (as a power of two) and sum: the result, or this split's part of it.
-template <typename T, int D>
-__device__ __forceinline__ void give(const CacheAttentionArgs &a, const Seq &s, int head, int group, int split, int row, int channel, float4v x, float m, float l, bool once)
+// Rows of one sequence and key head: row r is query head r % group of the r / group-th new token.  What all of them see,
+// taken together: steps of 64 keys from step0 on, of which keys all_begin to all_end - 1 are seen by each.
+struct Reach {
+    int rows, step0, steps, units, all_begin, all_end;  // units: steps, at least one where there are rows
+};
+__device__ __forceinline__ Reach reach(const CacheAttentionArgs &a, const Seq &s)
 {
-    const int t = (unsigned)row / (unsigned)group, h = head * group + (row - t * group);
-    const int64_t token = s.row + t, at = token * a.heads + h;
-    if (a.splits > 1) {
-        const int64_t all_rows = (int64_t)a.seq.M * a.heads;
-        *(float4v *)(a.partial + (split * all_rows + at) * D + channel) = x;
-        if (once) ((float2 *)(a.partial + a.splits * all_rows * D))[split * all_rows + at] = make_float2(m, l);
-        return;
-    }
-    const float f = l == 0.0f ? 0.0f : 1.0f / l;
-    *(uint2 *)((T *)a.out + token * a.ldo + (int64_t)h * D + channel) = make_uint2(Half<T>::pack(x[0] * f, x[1] * f), Half<T>::pack(x[2] * f, x[3] * f));
-    if (once && a.lse) a.lse[at] = kLn2 * (m + log2f(l));
+    const int group = a.heads / a.cache.heads, n = min(s.n, a.seq.max_new);
+    Reach r;
+    r.rows = n * group;
+    const int end = a.causal ? max(0, min(s.len, s.start + n)) : s.len, begin = a.window ? max(0, s.start - a.window + 1) : 0;
+    r.step0 = begin / kCacheTile;
+    r.steps = max(0, (end + kCacheTile - 1) / kCacheTile - r.step0);
+    r.units = n > 0 ? max(r.steps, 1) : 0;
+    r.all_end = a.causal ? min(s.len, s.start + 1) : s.len;
+    r.all_begin = a.window ? s.start + n - a.window : 0;
+    return r;
 }
 
-// Rows of one sequence and key head: row r is query head r % group of the r / group-th new token.  Here a workgroup has
-// NB * 16 of them, and its wavefronts take turns at the steps of 64 keys.
+// Four channels of a row, and once per row its maximum (as a power of two) and sum: the result, or the part of it that
+// `part` says is kept for the join.
+template <typename T, int D>
+__device__ __forceinline__ void give(const CacheAttentionArgs &a, const Seq &s, int head, int group, int64_t part, int row, int channel, float4v x, float m, float l, bool once)
+{
+    if (part >= 0) {
+        *(float4v *)(a.partial + part * D + channel) = x;
+        if (once) ((float2 *)(a.partial + a.part_rows * D))[part] = make_float2(m, l);
+        return;
+    }
+    const int t = (unsigned)row / (unsigned)group, h = head * group + (row - t * group);
+    const int64_t token = s.row + t;
+    const float f = l == 0.0f ? 0.0f : 1.0f / l;
+    *(uint2 *)((T *)a.out + token * a.ldo + (int64_t)h * D + channel) = make_uint2(Half<T>::pack(x[0] * f, x[1] * f), Half<T>::pack(x[2] * f, x[3] * f));
+    if (once && a.lse) a.lse[token * a.heads + h] = kLn2 * (m + log2f(l));
+}
+
+// units of all sequences before each, behind the parts
+__device__ __forceinline__ int *shares_of(const CacheAttentionArgs &a) { return (int *)(a.partial + a.part_rows * (a.cache.dim + 2)); }
+
+// Few rows: a workgroup has all NB * 16, and its wavefronts take turns at the steps of 64 keys.
 template <typename T, int D, int NB, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_cache_attention(CacheAttentionArgs a, int row_tiles)
+__global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_cache_attention(CacheAttentionArgs a)
 {
     constexpr int R = 16 * NB, KL = D / 64, NV = D / 16;
     typedef typename Mma<T>::Frag Frag;
@@ -99,217 +130,265 @@ __global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_c
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q16 = lane & 15, g = lane >> 4;
     const int H = a.cache.heads, group = a.heads / H;
 
-    unsigned i = blockIdx.x;
-    const int split = i % a.splits;
-    i /= a.splits;
-    const int bh = i % (a.seq.batch * H), head = bh % H, b = bh / H;
-    const int tile_of_rows = row_tiles - 1 - (int)(i / (a.seq.batch * H));  // causal rows at the end see most: first
-    const Seq s = sequence(a.seq, b);
-    const int total = min(s.n, a.seq.max_new) * group, first = tile_of_rows * R;  // the host keeps them below 2^31
-    if (first >= total) return;
-    const int last = min(first + R, total) - 1;
-
-    // keys that some row sees, and those that every row sees
-    const int t_first = (unsigned)first / (unsigned)group, t_last = (unsigned)last / (unsigned)group;
-    const int key_end = a.causal ? max(0, min(s.len, s.start + t_last + 1)) : s.len;
-    const int key_begin = a.window ? max(0, s.start + t_first - a.window + 1) : 0;
-    const int all_end = a.causal ? min(s.len, s.start + t_first + 1) : s.len, all_begin = a.window ? s.start + t_last - a.window + 1 : 0;
-    const int step0 = key_begin / kCacheTile, steps = max(0, (key_end + kCacheTile - 1) / kCacheTile - step0);
-    const int from = step0 + (unsigned)(steps * split) / (unsigned)a.splits, to = step0 + (unsigned)(steps * (split + 1)) / (unsigned)a.splits;
-
-    // this lane's query of each 16
-    int see_lo[NB], see_hi[NB];
-    Frag q[NB][2 * KL];
+    // This workgroup's part: one of a sequence's and head's `splits`, or its share of all steps of all sequences and heads in a
+    // row (lengths may differ, and only the device knows them).
+    int b, head, off = 0, left;
+    int64_t part = -1;
+    Seq s;
+    Reach see;
+    auto look_at = [&](int sequence_) { s = sequence(a.seq, sequence_), see = reach(a, s); };
+    if (a.share_log2 < 0) {
+        const int bh = blockIdx.x / a.splits, split = blockIdx.x - bh * a.splits;
+        b = bh / H, head = bh - b * H;
+        look_at(b);
+        off = (unsigned)(see.units * split) / (unsigned)a.splits;
+        left = (unsigned)(see.units * (split + 1)) / (unsigned)a.splits - off;
+        if (a.splits > 1) part = blockIdx.x;
+        if (left == 0) {  // fewer steps than splits: nothing to add
+            for (int at = threadIdx.x; at < see.rows * (D / 4); at += WAVES * 64)
+                give<T, D>(a, s, 0, 1, part * R + at / (D / 4), 0, at % (D / 4) * 4, float4v{}, -INFINITY, 0.0f, at % (D / 4) == 0);
+            return;
+        }
+    } else {
+        // every wavefront for itself: a lane has some of the sequences, in a row
+        const int each = (a.seq.batch + 63) / 64, b0 = min(lane * each, a.seq.batch), b1 = min(b0 + each, a.seq.batch);
+        int mine = 0;
+        for (int s = b0; s < b1; ++s) mine += reach(a, sequence(a.seq, s)).units;
+        int upto = mine;
+        if (each * 2 <= a.seq.batch) {  // more than one lane has any
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-        const int row = first + nb * 16 + q16;
-        const bool has = row < total;
-        const int t = has ? (unsigned)row / (unsigned)group : 0, h = head * group + (has ? row - t * group : 0);
-        see_hi[nb] = !has ? -1 : a.causal ? min(s.len - 1, s.start + t) : s.len - 1;
-        see_lo[nb] = a.window ? s.start + t - a.window + 1 : 0;
-        const T *x = (const T *)a.q + (s.row + t) * a.ldq + (int64_t)h * D;
-#pragma unroll
-        for (int j = 0; j < KL; ++j)
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-                if (has) q[nb][2 * j + hf] = *(const Frag *)(x + 64 * j + 16 * g + 8 * hf);
-                else q[nb][2 * j + hf] = Frag{};
+            for (int d = 1; d < 64; d *= 2) {
+                const int x = __shfl_up(upto, d);
+                if (lane >= d) upto += x;
             }
+        }
+        const int before = upto - mine, all = __builtin_amdgcn_readlane(upto, min(63, (a.seq.batch - 1) / each));
+        const uint64_t total = (uint64_t)all * H;  // below 2^31: the host's bound
+        const int u0 = (int)(blockIdx.x * total >> a.share_log2), u1 = (int)((blockIdx.x + 1) * total >> a.share_log2);
+        if (blockIdx.x == 0 && wave == 0) {  // for those who join the parts
+            int *const table = shares_of(a);
+            for (int s = b0, at = before; s < b1; ++s) {
+                table[s] = at;
+                at += reach(a, sequence(a.seq, s)).units;
+            }
+            if (lane == 0) table[a.seq.batch] = all;
+        }
+        if (u0 >= u1) return;
+        const int owner = __builtin_ctzll(__ballot(u0 < upto * H));  // the first lane whose sequences reach so far
+        int at = __builtin_amdgcn_readlane(before, owner);
+        for (b = owner * each;; ++b, at += see.units) {
+            look_at(b);
+            if (u0 < (at + see.units) * H) break;
+        }
+        off = u0 - at * H;
+        head = off / see.units, off -= head * see.units;
+        left = u1 - u0;
     }
 
-    float4v o[NB][NV] = {};
-    float m[NB], l[NB];
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) m[nb] = -INFINITY, l[nb] = 0.0f;
-    int eref = 0;
-    bool begun = false;
-    const int block_shift = a.cache.block >> 7;  // 64, 128, 256 tokens: 1, 2, 4 steps
-    const int key_row = 16 * (q16 >> 2) + (q16 & 3);  // + 4 b
+    for (;;) {
+        const int take = min(see.units - off, left);
+        if (a.share_log2 >= 0) part = take == see.units ? -1 : 2 * (int64_t)blockIdx.x + (off == 0);  // what began in another workgroup, or ends in one
+        const int total = see.rows, from = see.step0 + off, to = min(from + take, see.step0 + see.steps);
 
-    // Loads run ahead of what waits for them: a step's codes and scales are asked for one turn before, its block two turns
-    // before (the address depends on it).
-    uint4 kc[4][KL], vc[NV], kn[4][KL], vn[NV];
-    float ks_next = 0.0f, vs_next = 0.0f;
-    bool ok_next = false;
-    int page_next = -1;
-    auto page_of = [&](int step) { return a.seq.table[b * a.seq.ldt + (min(step, to - 1) >> block_shift)]; };
-    auto fetch = [&](int step) {
-        const int sub = step & ((1 << block_shift) - 1);
-        int page = __builtin_amdgcn_readfirstlane(page_next);
-        ok_next = page >= 0 && page < a.cache.blocks;
-        if (!ok_next) page = 0;
-        const int64_t unit = (int64_t)page * H + head;
-        const uint8_t *kp = a.cache.k + (unit * a.cache.block + sub * kCacheTile) * D;
-        const uint8_t *vp = a.cache.v + unit * D * a.cache.block + sub * kCacheTile;
-#pragma unroll
-        for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-            for (int j = 0; j < KL; ++j) kn[kb][j] = *(const uint4 *)(kp + (key_row + 4 * kb) * D + 64 * j + 16 * g);
-        ks_next = a.cache.k_scale[unit];
-        vs_next = a.cache.v_scale[unit];
-#pragma unroll
-        for (int n = 0; n < NV; ++n) vn[n] = *(const uint4 *)(vp + (16 * n + q16) * a.cache.block + 16 * g);
-        page_next = page_of(step + WAVES);
-    };
-    if (from + wave < to) {
-        page_next = page_of(from + wave);
-        fetch(from + wave);
-    }
-    for (int step = from + wave; step < to; step += WAVES) {
-#pragma unroll
-        for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-            for (int j = 0; j < KL; ++j) kc[kb][j] = kn[kb][j];
-#pragma unroll
-        for (int n = 0; n < NV; ++n) vc[n] = vn[n];
-        const float ks = ks_next, vs = vs_next;
-        const bool page_ok = ok_next;
-        if (step + WAVES < to) fetch(step + WAVES);
+        const int block_shift = a.cache.block >> 7;  // 64, 128, 256 tokens: 1, 2, 4 steps
+        const int key_row = 16 * (q16 >> 2) + (q16 & 3);  // + 4 b
 
-        float4v sc[NB][4] = {};
+        // A turn's loads all leave at once, and its block (the address depends on it) is asked for one turn before.  Keeping the
+        // next turn's codes in registers as well took longer (64 sequences of up to 8192 keys 119 us, 123 with them).
+        struct Turn {
+            uint4 k[4][KL], v[NV];
+            float ks, vs;
+            int page;
+            bool ok;
+        };
+        auto page_of = [&](int step) { return a.seq.table[b * a.seq.ldt + (min(step, to - 1) >> block_shift)]; };
+        auto fetch = [&](Turn &x, int step) {
+            const int sub = step & ((1 << block_shift) - 1);
+            int page = __builtin_amdgcn_readfirstlane(x.page);
+            x.page = page_of(step + WAVES);
+            x.ok = page >= 0 && page < a.cache.blocks;
+            if (!x.ok) page = 0;
+            const int64_t unit = (int64_t)page * H + head;
+            const uint8_t *kp = a.cache.k + (unit * a.cache.block + sub * kCacheTile) * D;
+            const uint8_t *vp = a.cache.v + unit * D * a.cache.block + sub * kCacheTile;
+            x.ks = a.cache.k_scale[unit];
+            x.vs = a.cache.v_scale[unit];
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb)
+            for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
-            for (int j = 0; j < KL; ++j) {
-                const Frag k0 = widen<T>(kc[kb][j].x, kc[kb][j].y), k1 = widen<T>(kc[kb][j].z, kc[kb][j].w);
+                for (int j = 0; j < KL; ++j) x.k[kb][j] = load_once(kp + (key_row + 4 * kb) * D + 64 * j + 16 * g);
+#pragma unroll
+            for (int n = 0; n < NV; ++n) x.v[n] = load_once(vp + (16 * n + q16) * a.cache.block + 16 * g);
+        };
+        Turn turn;
+        turn.page = from + wave < to ? page_of(from + wave) : -1;
+
+        // this lane's query of each 16
+        int see_lo[NB], see_hi[NB];
+        Frag q[NB][2 * KL];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const int row = nb * 16 + q16;
+            const bool has = row < total;
+            const int t = has ? (unsigned)row / (unsigned)group : 0, h = head * group + (has ? row - t * group : 0);
+            see_hi[nb] = !has ? -1 : a.causal ? min(s.len - 1, s.start + t) : s.len - 1;
+            see_lo[nb] = a.window ? s.start + t - a.window + 1 : 0;
+            const T *x = (const T *)a.q + (s.row + t) * a.ldq + (int64_t)h * D;
+#pragma unroll
+            for (int j = 0; j < KL; ++j)
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf) {
+                    if (has) q[nb][2 * j + hf] = *(const Frag *)(x + 64 * j + 16 * g + 8 * hf);
+                    else q[nb][2 * j + hf] = Frag{};
+                }
+        }
+
+        float4v o[NB][NV] = {};
+        float m[NB], l[NB];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) m[nb] = -INFINITY, l[nb] = 0.0f;
+        int eref = 0;
+        bool begun = false;
+        auto compute = [&](Turn &x, int step) {
+            float4v sc[NB][4] = {};
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+                for (int j = 0; j < KL; ++j) {
+                    const Frag k0 = widen<T>(x.k[kb][j].x, x.k[kb][j].y), k1 = widen<T>(x.k[kb][j].z, x.k[kb][j].w);
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) {
+                        sc[nb][kb] = Mma<T>::mma(k0, q[nb][2 * j], sc[nb][kb]);
+                        sc[nb][kb] = Mma<T>::mma(k1, q[nb][2 * j + 1], sc[nb][kb]);
+                    }
+                }
+
+            const int key0 = step * kCacheTile + 16 * g;  // this lane's first key
+            if (!x.ok || (step + 1) * kCacheTile > see.all_end || step * kCacheTile < see.all_begin) {
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
-                    sc[nb][kb] = Mma<T>::mma(k0, q[nb][2 * j], sc[nb][kb]);
-                    sc[nb][kb] = Mma<T>::mma(k1, q[nb][2 * j + 1], sc[nb][kb]);
+                    const int hi = x.ok ? see_hi[nb] : -1, lo = see_lo[nb];
+#pragma unroll
+                    for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const int key = key0 + 4 * kb + r;
+                            sc[nb][kb][r] = ((key > hi) | (key < lo)) ? -INFINITY : sc[nb][kb][r];
+                        }
                 }
             }
+            // a slot behind the sequence holds anything, a NaN too: its weight 0 does not hide that
+            if (!x.ok || (step + 1) * kCacheTile > s.len) {
+                const int valid = x.ok ? s.len - key0 : 0;
+#pragma unroll
+                for (int n = 0; n < NV; ++n)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const int bytes = min(max(valid - 4 * w, 0), 4);
+                        (&x.v[n].x)[w] &= bytes == 4 ? 0xffffffffu : (1u << (8 * bytes)) - 1;
+                    }
+            }
 
-        const int key0 = step * kCacheTile + 16 * g;  // this lane's first key
-        if (!page_ok || (step + 1) * kCacheTile > all_end || step * kCacheTile < all_begin) {
+            const float c = fmaxf(a.alpha * kLog2e * x.ks, 1.17549435e-38f);
+            const int ev = __builtin_amdgcn_readfirstlane(exponent_of(x.vs));
+            if (!begun) eref = ev, begun = true;
+            if (ev - eref > kDrift || eref - ev > kDrift) {
+                const float f = pow2(eref - ev);
+                eref = ev;
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int n = 0; n < NV; ++n) o[nb][n] *= f;
+            }
+            const float drift = (float)(ev - eref), undrift = pow2(eref - ev);
+            half8 p[NB][2];
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
-                const int hi = page_ok ? see_hi[nb] : -1, lo = see_lo[nb];
+                float top = most(most(sc[nb][0][0], sc[nb][0][1]), most(sc[nb][0][2], sc[nb][0][3]));
+#pragma unroll
+                for (int kb = 1; kb < 4; ++kb) top = most(most(top, most(sc[nb][kb][0], sc[nb][kb][1])), most(sc[nb][kb][2], sc[nb][kb][3]));
+                top *= c;
+                if (__any(top > m[nb] + kSlack)) {
+                    const float now = fmaxf(m[nb], max_of_query(top));
+                    const float f = m[nb] == -INFINITY ? 0.0f : exp2f(m[nb] - now);
+                    m[nb] = now;
+                    l[nb] *= f;
+#pragma unroll
+                    for (int n = 0; n < NV; ++n) o[nb][n] *= f;
+                }
+                const float base = (m[nb] == -INFINITY ? 0.0f : m[nb]) - drift;
+                float sum = 0.0f, w[16];
 #pragma unroll
                 for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        const int key = key0 + 4 * kb + r;
-                        sc[nb][kb][r] = ((key > hi) | (key < lo)) ? -INFINITY : sc[nb][kb][r];
+                        w[4 * kb + r] = __builtin_amdgcn_exp2f(fmaf(sc[nb][kb][r], c, -base));
+                        sum += w[4 * kb + r];
                     }
+                l[nb] = fmaf(sum, undrift, l[nb]);
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf)
+                    p[nb][hf] = half8{(_Float16)w[8 * hf], (_Float16)w[8 * hf + 1], (_Float16)w[8 * hf + 2], (_Float16)w[8 * hf + 3],
+                                      (_Float16)w[8 * hf + 4], (_Float16)w[8 * hf + 5], (_Float16)w[8 * hf + 6], (_Float16)w[8 * hf + 7]};
             }
-        }
-        // a slot behind the sequence holds anything, a NaN too: its weight 0 does not hide that
-        if (!page_ok || (step + 1) * kCacheTile > s.len) {
-            const int valid = page_ok ? s.len - key0 : 0;
 #pragma unroll
-            for (int n = 0; n < NV; ++n)
+            for (int n = 0; n < NV; ++n) {
+                const half8 v0 = widen<_Float16>(x.v[n].x, x.v[n].y), v1 = widen<_Float16>(x.v[n].z, x.v[n].w);
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const int bytes = min(max(valid - 4 * w, 0), 4);
-                    (&vc[n].x)[w] &= bytes == 4 ? 0xffffffffu : (1u << (8 * bytes)) - 1;
+                for (int nb = 0; nb < NB; ++nb) {
+                    o[nb][n] = Mma<_Float16>::mma(v0, p[nb][0], o[nb][n]);
+                    o[nb][n] = Mma<_Float16>::mma(v1, p[nb][1], o[nb][n]);
                 }
+            }
+        };
+        for (int step = from + wave; step < to; step += WAVES) {
+            fetch(turn, step);
+            compute(turn, step);
         }
 
-        const float c = fmaxf(a.alpha * kLog2e * ks, 1.17549435e-38f);
-        const int ev = __builtin_amdgcn_readfirstlane(exponent_of(vs));
-        if (!begun) eref = ev, begun = true;
-        if (ev - eref > kDrift || eref - ev > kDrift) {
-            const float f = pow2(eref - ev);
-            eref = ev;
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-                for (int n = 0; n < NV; ++n) o[nb][n] *= f;
-        }
-        const float drift = (float)(ev - eref), undrift = pow2(eref - ev);
-        half8 p[NB][2];
+        // o[nb][n][r]: query q16 of the nb-th 16, channel 16 n + 4 g + r, in units of 2^eref
+        const float unit = pow2(eref);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-            float top = most(most(sc[nb][0][0], sc[nb][0][1]), most(sc[nb][0][2], sc[nb][0][3]));
+            l[nb] = sum_of_query(l[nb]);
 #pragma unroll
-            for (int kb = 1; kb < 4; ++kb) top = most(most(top, most(sc[nb][kb][0], sc[nb][kb][1])), most(sc[nb][kb][2], sc[nb][kb][3]));
-            top *= c;
-            if (__any(top > m[nb] + kSlack)) {
-                const float now = fmaxf(m[nb], max_of_query(top));
-                const float f = m[nb] == -INFINITY ? 0.0f : exp2f(m[nb] - now);
-                m[nb] = now;
-                l[nb] *= f;
-#pragma unroll
-                for (int n = 0; n < NV; ++n) o[nb][n] *= f;
-            }
-            const float base = (m[nb] == -INFINITY ? 0.0f : m[nb]) - drift;
-            float sum = 0.0f, w[16];
-#pragma unroll
-            for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    w[4 * kb + r] = __builtin_amdgcn_exp2f(fmaf(sc[nb][kb][r], c, -base));
-                    sum += w[4 * kb + r];
-                }
-            l[nb] = fmaf(sum, undrift, l[nb]);
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf)
-                p[nb][hf] = half8{(_Float16)w[8 * hf], (_Float16)w[8 * hf + 1], (_Float16)w[8 * hf + 2], (_Float16)w[8 * hf + 3],
-                                  (_Float16)w[8 * hf + 4], (_Float16)w[8 * hf + 5], (_Float16)w[8 * hf + 6], (_Float16)w[8 * hf + 7]};
+            for (int n = 0; n < NV; ++n) o[nb][n] *= unit;
         }
 #pragma unroll
-        for (int n = 0; n < NV; ++n) {
-            const half8 v0 = widen<_Float16>(vc[n].x, vc[n].y), v1 = widen<_Float16>(vc[n].z, vc[n].w);
+        for (int nb = 0; nb < NB; ++nb) {
+            const int at = wave * R + nb * 16 + q16;
+            if (g == 0) merged_ml[at] = make_float2(m[nb], l[nb]);
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                o[nb][n] = Mma<_Float16>::mma(v0, p[nb][0], o[nb][n]);
-                o[nb][n] = Mma<_Float16>::mma(v1, p[nb][1], o[nb][n]);
-            }
+            for (int n = 0; n < NV; ++n) merged[at * (D / 4) + 4 * n + g] = make_float4(o[nb][n][0], o[nb][n][1], o[nb][n][2], o[nb][n][3]);
         }
-    }
+        __syncthreads();
+        for (int at = threadIdx.x; at < R * (D / 4); at += WAVES * 64) {
+            const int r = at / (D / 4);
+            if (r >= total) continue;
+            float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) top = fmaxf(top, merged_ml[w * R + r].x);
+            float4v x = {};
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                const float2 ml = merged_ml[w * R + r];
+                const float f = ml.x == -INFINITY && ml.y == 0.0f ? 0.0f : exp2f(ml.x - top);  // a NaN among the scores stays one
+                const float4 y = merged[w * R * (D / 4) + at];
+                x += float4v{y.x, y.y, y.z, y.w} * f;
+                sum = fmaf(ml.y, f, sum);
+            }
+            give<T, D>(a, s, head, group, part < 0 ? -1 : part * R + r, r, at % (D / 4) * 4, x, top, sum, at % (D / 4) == 0);
+        }
 
-    // o[nb][n][r]: query q16 of the nb-th 16, channel 16 n + 4 g + r, in units of 2^eref
-    const float unit = pow2(eref);
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-        l[nb] = sum_of_query(l[nb]);
-#pragma unroll
-        for (int n = 0; n < NV; ++n) o[nb][n] *= unit;
-    }
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-        const int at = wave * R + nb * 16 + q16;
-        if (g == 0) merged_ml[at] = make_float2(m[nb], l[nb]);
-#pragma unroll
-        for (int n = 0; n < NV; ++n) merged[at * (D / 4) + 4 * n + g] = make_float4(o[nb][n][0], o[nb][n][1], o[nb][n][2], o[nb][n][3]);
-    }
-    __syncthreads();
-    for (int at = threadIdx.x; at < R * (D / 4); at += WAVES * 64) {
-        const int r = at / (D / 4);
-        if (first + r >= total) continue;
-        float top = -INFINITY, sum = 0.0f;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, merged_ml[w * R + r].x);
-        float4v x = {};
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            const float2 ml = merged_ml[w * R + r];
-            const float f = ml.x == -INFINITY && ml.y == 0.0f ? 0.0f : exp2f(ml.x - top);  // a NaN among the scores stays one
-            const float4 y = merged[w * R * (D / 4) + at];
-            x += float4v{y.x, y.y, y.z, y.w} * f;
-            sum = fmaf(ml.y, f, sum);
+        left -= take, off += take;
+        if (left == 0) break;
+        off = 0;  // another workgroup's share ends inside a head's steps, this one's goes on with the next
+        if (++head == H) {
+            head = 0;
+            do look_at(++b);
+            while (see.units == 0);
         }
-        give<T, D>(a, s, head, group, split, first + r, at % (D / 4) * 4, x, top, sum, at % (D / 4) == 0);
+        __syncthreads();  // before the next part's sums
     }
 }
 
@@ -585,117 +664,137 @@ __global__ __launch_bounds__(GROUPS * 256, D <= 128 ? 2 : 1) void k_cache_attent
             for (int r = 0; r < 4; ++r) x[n][r] = x[n][r] * f + sums[(n * 4 + r) * NT + tid] * g;
     }
     if (!has) return;
+    const int64_t part = a.splits > 1 ? split * (int64_t)a.seq.M * a.heads + (s.row + token) * a.heads + head * group + row - token * group : -1;
 #pragma unroll
     for (int n = 0; n < DN; ++n)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) give<T, D>(a, s, head, group, split, row, 32 * n + 8 * r + 4 * h2, x[n][r], m, l, n == 0 && r == 0 && h2 == 0);
+        for (int r = 0; r < 4; ++r) give<T, D>(a, s, head, group, part, row, 32 * n + 8 * r + 4 * h2, x[n][r], m, l, n == 0 && r == 0 && h2 == 0);
 }
 
 // The parts of a row: D / 4 threads have four channels each, ALONE of them a row for themselves (few parts, many rows), or
 // all of a workgroup's threads one row, each D / 4 some of its parts.
-constexpr int kMostSplits = 128, kFewSplits = 8;
+constexpr int kFewSplits = 8, kMostParts = 1024;
 template <typename T, int D, bool ALONE>
 __global__ __launch_bounds__(256) void k_cache_attention_join(CacheAttentionArgs a)
 {
     constexpr int C = D / 4, kSide = 256 / C;
-    __shared__ float weight[ALONE ? 1 : kMostSplits], total[2];
+    __shared__ float weight[ALONE ? 1 : kMostParts], some[2][4];
     __shared__ float4v side[ALONE ? 1 : kSide][C];
     const int tid = threadIdx.x, c = tid % C, nth = tid / C;
     const unsigned item = ALONE ? blockIdx.x * kSide + nth : blockIdx.x, bt = item / a.heads;
     const int h = item % a.heads, b = bt / a.seq.max_new, t = bt % a.seq.max_new;
     if (ALONE && b >= a.seq.batch) return;
+    const bool shared = !ALONE && a.share_log2 >= 0;
+    int units = 0, units_before = 0, units_all = 0;
+    if (shared) {
+        const int *const shares = shares_of(a);
+        units_before = shares[b], units = shares[b + 1] - units_before, units_all = shares[a.seq.batch];
+    }
     const Seq s = sequence(a.seq, b);
     if (t >= s.n) return;
-    const int64_t all_rows = (int64_t)a.seq.M * a.heads, row = (int64_t)(s.row + t) * a.heads + h;
-    const float2 *ml = (const float2 *)(a.partial + a.splits * all_rows * D) + row;
-    const float *o = a.partial + row * D + 4 * c;
+    const int64_t row = (int64_t)(s.row + t) * a.heads + h;
+    // the row's parts: the first, and from the second on every `stride`-th
+    const int H = a.cache.heads, group = a.heads / H, r = t * group + h % group;
+    int64_t first = row, stride = (int64_t)a.seq.M * a.heads;
+    if (a.share_rows <= 32) first = ((int64_t)(b * H + h / group) * a.splits) * a.share_rows + r, stride = a.share_rows;
+    int64_t second = first + stride;
+    int parts = a.splits;
+    if (shared) {
+        const int u = units_before * H + h / group * units;
+        const uint64_t total = (uint64_t)units_all * H;
+        auto owner = [&](int x) {  // the workgroup whose share holds unit x; the quotient is at most one off
+            int w = (int)(((double)x + 0.5) * (double)(1 << a.share_log2) / (double)total);
+            if ((int)((uint64_t)w * total >> a.share_log2) > x) --w;
+            if ((int)((uint64_t)(w + 1) * total >> a.share_log2) <= x) ++w;
+            return w;
+        };
+        const int w0 = owner(u), w1 = owner(u + units - 1);
+        if (w0 == w1) return;  // has been written whole
+        parts = w1 - w0 + 1;
+        first = (int64_t)(2 * w0 + 1) * a.share_rows + r;
+        second = (int64_t)(2 * w0 + 2) * a.share_rows + r, stride = 2 * a.share_rows;
+    }
+    auto at = [&](int k) { return k == 0 ? first : second + (k - 1) * stride; };
+    const float2 *const ml = (const float2 *)(a.partial + a.part_rows * D);
+    const float *const o = a.partial + 4 * c;
     float4v x = {};
     float top = -INFINITY, sum = 0.0f;
+    auto factor = [&](float2 p) { return p.x == -INFINITY && p.y == 0.0f ? 0.0f : exp2f(p.x - top); };  // a NaN among the scores stays one
     if constexpr (ALONE) {
         float2 p[kFewSplits];
 #pragma unroll
         for (int k = 0; k < kFewSplits; ++k) {
-            p[k] = k < a.splits ? ml[k * all_rows] : make_float2(-INFINITY, 0.0f);
+            p[k] = k < parts ? ml[at(k)] : make_float2(-INFINITY, 0.0f);
             top = fmaxf(top, p[k].x);
         }
 #pragma unroll
         for (int k = 0; k < kFewSplits; ++k) {
-            if (k >= a.splits) break;
-            const float f = p[k].x == -INFINITY && p[k].y == 0.0f ? 0.0f : exp2f(p[k].x - top);  // a NaN among the scores stays one
+            if (k >= parts) break;
+            const float f = factor(p[k]);
             sum = fmaf(f, p[k].y, sum);
-            x += *(const float4v *)(o + k * all_rows * D) * f;
+            x += *(const float4v *)(o + at(k) * D) * f;
         }
     } else {
-        if (tid < 64) {
-            float2 p[kMostSplits / 64];
+        float2 p[kMostParts / 256];
 #pragma unroll
-            for (int j = 0; j < kMostSplits / 64; ++j) {
-                p[j] = tid + 64 * j < a.splits ? ml[(tid + 64 * j) * all_rows] : make_float2(-INFINITY, 0.0f);
-                top = fmaxf(top, p[j].x);
-            }
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-#pragma unroll
-            for (int j = 0; j < kMostSplits / 64; ++j) {
-                const float f = p[j].x == -INFINITY && p[j].y == 0.0f ? 0.0f : exp2f(p[j].x - top);
-                weight[tid + 64 * j] = f;
-                sum = fmaf(f, p[j].y, sum);
-            }
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-            if (tid == 0) total[0] = top, total[1] = sum;
+        for (int j = 0; j < kMostParts / 256; ++j) {
+            p[j] = tid + 256 * j < parts ? ml[at(tid + 256 * j)] : make_float2(-INFINITY, 0.0f);
+            top = fmaxf(top, p[j].x);
         }
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+        if ((tid & 63) == 0) some[0][tid >> 6] = top;
         __syncthreads();
+        top = fmaxf(fmaxf(some[0][0], some[0][1]), fmaxf(some[0][2], some[0][3]));
+#pragma unroll
+        for (int j = 0; j < kMostParts / 256; ++j) {
+            const float f = factor(p[j]);
+            weight[tid + 256 * j] = f;
+            sum = fmaf(f, p[j].y, sum);
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+        if ((tid & 63) == 0) some[1][tid >> 6] = sum;
+        __syncthreads();
+        sum = (some[1][0] + some[1][1]) + (some[1][2] + some[1][3]);
 #pragma unroll 4
-        for (int k = nth; k < a.splits; k += kSide) x += *(const float4v *)(o + k * all_rows * D) * weight[k];
+        for (int k = nth; k < parts; k += kSide) x += *(const float4v *)(o + at(k) * D) * weight[k];
         side[nth][c] = x;
         __syncthreads();
         if (nth) return;
 #pragma unroll
         for (int k = 1; k < kSide; ++k) x += side[k][c];
-        top = total[0], sum = total[1];
     }
     const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
     *(uint2 *)((T *)a.out + (s.row + t) * a.ldo + (int64_t)h * D + 4 * c) = make_uint2(Half<T>::pack(x[0] * f, x[1] * f), Half<T>::pack(x[2] * f, x[3] * f));
     if (c == 0 && a.lse) a.lse[row] = kLn2 * (top + log2f(sum));
 }
 
-// Rows a workgroup takes: up to 16 or 32 that its four wavefronts share, else 32 for each of four (or of twice four).
-struct Shape {
-    int rows;
-    bool shared;
-};
-Shape shape_of(int64_t rows, int dim)
-{
-    if (rows <= 16) return {16, true};
-    if (rows <= 32 && dim < 256) return {32, true};
-    return {128, false};
-}
 constexpr int kAttWaves = 4;
 
 template <typename T, int D>
-void launch(const CacheAttentionArgs &a, const Shape &shape, int row_tiles, int64_t groups, hipStream_t st)
+void launch(const CacheAttentionArgs &a, const AttentionPlan &plan, hipStream_t st)
 {
     constexpr int NB = D < 256 ? 2 : 1;
-    const dim3 grid((unsigned)groups), block(kAttWaves * 64);
-    if (!shape.shared) {
+    const dim3 grid((unsigned)plan.groups), block(kAttWaves * 64);
+    if (plan.rows > 32) {
         // Two workgroups' worth of wavefronts on the same rows halve the way of the rows that see most, which is what few
         // workgroups take their time for; many balance by themselves, unless long sequences of a batch differ.  us, one / two,
         // heads of 128: a causal prompt of 2048 with 32 heads 58 / 55, two of them 95 / 109; 128 rows over 256 keys, 32 times,
         // 40 / 56; chunks of up to 1024 tokens over 5163 to 16024 keys, four times, 641 / 610.
         constexpr int kMost = D <= 128 ? 2 : 1;
         const bool differ = a.seq.batch > 1 && a.seq.max_len >= 8192;
-        if (kMost == 2 && a.seq.max_len >= 1024 && groups <= (differ ? 1024 : 512))
-            hipLaunchKernelGGL((k_cache_attention_rows<T, D, kMost>), grid, dim3(kMost * 256), 0, st, a, row_tiles);
+        if (kMost == 2 && a.seq.max_len >= 1024 && plan.groups <= (differ ? 1024 : 512))
+            hipLaunchKernelGGL((k_cache_attention_rows<T, D, kMost>), grid, dim3(kMost * 256), 0, st, a, plan.row_tiles);
         else
-            hipLaunchKernelGGL((k_cache_attention_rows<T, D, 1>), grid, block, 0, st, a, row_tiles);
-    } else if (shape.rows == 16)
-        hipLaunchKernelGGL((k_cache_attention<T, D, 1, kAttWaves>), grid, block, 0, st, a, row_tiles);
+            hipLaunchKernelGGL((k_cache_attention_rows<T, D, 1>), grid, block, 0, st, a, plan.row_tiles);
+    } else if (plan.rows == 16)
+        hipLaunchKernelGGL((k_cache_attention<T, D, 1, kAttWaves>), grid, block, 0, st, a);
     else
-        hipLaunchKernelGGL((k_cache_attention<T, D, NB, kAttWaves>), grid, block, 0, st, a, row_tiles);
-    if (a.splits > 1) {
+        hipLaunchKernelGGL((k_cache_attention<T, D, NB, kAttWaves>), grid, block, 0, st, a);
+    if (plan.workspace) {
         const int64_t rows = (int64_t)a.seq.batch * a.seq.max_new * a.heads, alone = 256 / (D / 4);
-        if (a.splits <= kFewSplits)
+        if (a.splits > 1 && a.splits <= kFewSplits)
             hipLaunchKernelGGL((k_cache_attention_join<T, D, true>), dim3((unsigned)((rows + alone - 1) / alone)), block, 0, st, a);
         else
             hipLaunchKernelGGL((k_cache_attention_join<T, D, false>), dim3((unsigned)rows), block, 0, st, a);
@@ -703,45 +802,67 @@ void launch(const CacheAttentionArgs &a, const Shape &shape, int row_tiles, int6
 }
 
 template <typename T>
-void launch_type(const CacheAttentionArgs &a, const Shape &shape, int row_tiles, int64_t groups, hipStream_t st)
+void launch_type(const CacheAttentionArgs &a, const AttentionPlan &plan, hipStream_t st)
 {
-    if (a.cache.dim == 64) launch<T, 64>(a, shape, row_tiles, groups, st);
-    else if (a.cache.dim == 128) launch<T, 128>(a, shape, row_tiles, groups, st);
-    else launch<T, 256>(a, shape, row_tiles, groups, st);
+    if (a.cache.dim == 64) launch<T, 64>(a, plan, st);
+    else if (a.cache.dim == 128) launch<T, 128>(a, plan, st);
+    else launch<T, 256>(a, plan, st);
 }
 
 }  // namespace
 
-double cache_attention_groups(int batch, int heads, int kv_heads, int dim, int max_new, int splits)
+AttentionPlan cache_attention_plan(int M, int heads, int kv_heads, int dim, int batch, int max_new, int max_len)
 {
-    const int64_t rows = (int64_t)max_new * (heads / kv_heads);
-    const Shape shape = shape_of(rows, dim);
-    return (double)((rows + shape.rows - 1) / shape.rows) * batch * kv_heads * splits;
+    AttentionPlan p{};
+    const int64_t rows = (int64_t)max_new * (heads / kv_heads), steps = ((int64_t)max_len + kCacheTile - 1) / kCacheTile;
+    const double parts = (double)batch * kv_heads;  // sequences times key heads
+    // rows of a workgroup: up to 16 or 32 that its four wavefronts share, else 32 for each of four (or of twice four)
+    p.rows = rows <= 16 ? 16 : rows <= 32 && dim < 256 ? 32 : 128;
+    p.row_tiles = (int)((rows + p.rows - 1) / p.rows);
+    p.groups = (double)p.row_tiles * parts;
+    p.splits = 1, p.share_log2 = -1;
+    if (p.rows <= 32) {
+        // Two workgroups for every compute unit, as long as each of their wavefronts still has a step: every sequence is split
+        // into as many parts, and a long one's take longer, which is little where they are short (us, a token over 131072 keys
+        // 49.5, in equal shares of all steps 51.8; 32 sequences of up to 3000 keys in a whole decode step 41 and 46) ...
+        const double all = parts * (double)steps;
+        const int64_t want = parts >= 512 ? 1 : (int64_t)((512 + parts - 1) / parts), most_splits = steps / kAttWaves;
+        const int64_t splits = want < most_splits ? want : most_splits > 1 ? most_splits : 1;
+        if (steps <= 8 * kAttWaves * splits || all >= (double)(1u << 31)) {
+            if (splits > 1) {
+                p.splits = (int)splits;
+                p.groups *= (double)splits;
+                p.part_rows = (int64_t)p.groups * p.rows;
+                p.workspace = (size_t)p.part_rows * (dim + 2) * sizeof(float);
+            }
+            return p;
+        }
+        // ... and else everybody gets as many steps (64 sequences of up to 8192 keys 127 and 122): two workgroups for every
+        // compute unit, four where sequences and heads are that many.
+        const double full = parts >= 1024 ? kMostParts : 512, most = all / 4 < full ? all / 4 : full;
+        while ((double)(1 << (p.share_log2 + 1)) <= most) ++p.share_log2;
+        p.groups = 1 << p.share_log2;
+        p.part_rows = (int64_t)2 * p.rows << p.share_log2;
+        p.workspace = (size_t)p.part_rows * (dim + 2) * sizeof(float) + ((size_t)batch + 1) * sizeof(int);
+        return p;
+    }
+    // Parts of many rows are large: only for a workgroup on every compute unit, and of 16 steps at least.
+    const int64_t want = p.groups >= 256 ? 1 : (int64_t)((256 + p.groups - 1) / p.groups), most = steps / 16, s = want < most ? want : most;
+    if (s <= 1) return p;
+    p.splits = (int)s;
+    p.groups *= p.splits;
+    p.part_rows = (int64_t)p.splits * M * heads;
+    p.workspace = (size_t)p.part_rows * (dim + 2) * sizeof(float);
+    return p;
 }
 
-int cache_attention_splits(int batch, int heads, int kv_heads, int dim, int max_new, int max_len)
+hipError_t launch_cache_attention(CacheAttentionArgs a, const AttentionPlan &plan, hipStream_t st)
 {
-    const int64_t rows = (int64_t)max_new * (heads / kv_heads);
-    const Shape shape = shape_of(rows, dim);
-    const double groups = cache_attention_groups(batch, heads, kv_heads, dim, max_new, 1);
-    const int64_t steps = ((int64_t)max_len + kCacheTile - 1) / kCacheTile;
-    // Four workgroups for every compute unit, as long as each of their wavefronts still has a few steps; of many rows, whose
-    // parts are large, one, with 16 steps at least.
-    const int64_t full = shape.shared ? 1024 : 256, want = groups >= full ? 1 : (int64_t)((full + groups - 1) / groups), most = steps / (shape.shared ? kAttWaves : 16);
-    const int64_t s = want < most ? want : most;
-    return (int)(s < 1 ? 1 : s > kMostSplits ? kMostSplits : s);
-}
-
-hipError_t launch_cache_attention(const CacheAttentionArgs &a, hipStream_t st)
-{
-    const int64_t rows = (int64_t)a.seq.max_new * (a.heads / a.cache.heads);
-    const Shape shape = shape_of(rows, a.cache.dim);
-    const int row_tiles = (int)((rows + shape.rows - 1) / shape.rows);
-    const int64_t groups = (int64_t)row_tiles * a.seq.batch * a.cache.heads * a.splits;
+    a.splits = plan.splits, a.share_log2 = plan.share_log2, a.share_rows = plan.rows, a.part_rows = plan.part_rows;
     if (a.bf16)
-        launch_type<__bf16>(a, shape, row_tiles, groups, st);
+        launch_type<__bf16>(a, plan, st);
     else
-        launch_type<_Float16>(a, shape, row_tiles, groups, st);
+        launch_type<_Float16>(a, plan, st);
     return hipGetLastError();
 }
 

@@ -118,7 +118,8 @@ def test_workspace_sizes():
     assert f(M=8192, batch=1, max_new=8192, max_len=8192, **kw) == 0   # enough rows
     n = f(M=1, batch=1, max_new=1, max_len=131072, **kw)
     assert n > 0 and n % 256 == 0 and n >= 2 * 32 * 130 * 4
-    assert f(M=3, batch=1, max_new=1, max_len=131072, **kw) >= 3 * (n - 256)
+    m = f(M=300, batch=1, max_new=300, max_len=131072, **kw)           # many rows: parts of each
+    assert m % 256 == 0 and m >= 2 * 300 * 32 * 130 * 4
     assert f(M=1, batch=1, max_new=1, max_len=1000, heads=3, kv_heads=2, dim=128) == 0
 
 
