@@ -119,9 +119,10 @@ _lib.bwta_prepare_act_autoscale.argtypes = [_P, _c.c_int64, _c.c_int, _c.c_int, 
 
 
 class Cache(_c.Structure):
-    """bwta_cache of bwta.h.  `tensors` keeps what the addresses point to alive (see make_cache)."""
+    """bwta_cache of bwta.h, and behind it one more than the number of its tensors' device (0: not known).  `tensors` keeps what the
+    addresses point to alive (see make_cache)."""
     _fields_ = [("k", _P), ("v", _P), ("k_scale", _P), ("v_scale", _P), ("blocks", _c.c_int32), ("kv_heads", _c.c_int32),
-                ("block", _c.c_int32), ("dim", _c.c_int32)]
+                ("block", _c.c_int32), ("dim", _c.c_int32), ("place", _c.c_int32)]
 
 
 _CP = _c.POINTER(Cache)
@@ -439,6 +440,15 @@ def _dtype(x, dtype):
         raise TypeError("pass dtype= with addresses; tensors are float16 or bfloat16, got %s" % getattr(x, "dtype", type(x).__name__)) from None
 
 
+def _here(*xs):
+    """These calls launch on the current device: tensors have to be there."""
+    for x in xs:
+        if isinstance(x, torch.Tensor) and not (x.is_cuda and x.get_device() == torch.cuda.current_device()):
+            raise ValueError("a tensor on %s, the current device is %s" % (x.device, torch.cuda.current_device() if torch.cuda.is_available() else "none"))
+        if isinstance(x, Cache) and x.place > 0 and x.place - 1 != torch.cuda.current_device():
+            raise ValueError("a cache on device %d, the current one is %d" % (x.place - 1, torch.cuda.current_device()))
+
+
 def make_cache(k, v, k_scale, v_scale, *, blocks=None, kv_heads=None, block=None, dim=None):
     """The cache of 8-bit keys and values as the calls below take it (build once, reuse).  k [blocks, kv_heads, block, dim]
     and v [blocks, kv_heads, dim, block] are contiguous tensors of one byte an element (uint8 or float8_e4m3fn), k_scale and
@@ -457,7 +467,8 @@ def make_cache(k, v, k_scale, v_scale, *, blocks=None, kv_heads=None, block=None
         if any(g is not None and g != s for g, s in zip(given, sizes)):
             raise ValueError("sizes %s given, the tensors have %s" % (given, sizes))
         blocks, kv_heads, block, dim = sizes
-    c = Cache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), blocks, kv_heads, block, dim)
+    place = k.get_device() + 1 if isinstance(k, torch.Tensor) else 0
+    c = Cache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), blocks, kv_heads, block, dim, place)
     c.tensors = (k, v, k_scale, v_scale)
     return c
 
@@ -465,6 +476,7 @@ def make_cache(k, v, k_scale, v_scale, *, blocks=None, kv_heads=None, block=None
 def bwta_head_norm_rope(Q, K, wq, wk, positions, inv_freq, Qout, Kout, *, M, heads, kv_heads, dim, rot_dim=None, eps=1e-6,
                         norm=True, interleaved=False, ldq=None, ldk=None, ldqo=None, ldko=None, dtype=None, stream=None):
     """rot_dim: all of dim unless given.  norm: whether heads are normalised (weights None: by 1)."""
+    _here(Q, K, wq, wk, positions, inv_freq, Qout, Kout)
     ldq = heads * dim if ldq is None else ldq
     ldk = kv_heads * dim if ldk is None else ldk
     _check(_lib.bwta_head_norm_rope(_ptr(Q), ldq, heads, _ptr(wq), _ptr(K), ldk, kv_heads, _ptr(wk), _dtype(K if Q is None else Q, dtype),
@@ -480,6 +492,7 @@ def _ldt(table, given):
 
 
 def _cache_rows(call, cache, K, V, table, lens, cu, M, batch, max_new, max_len, ldk, ldv, ldt, dtype, stream):
+    _here(cache, K, V, table, lens, cu)
     width = cache.kv_heads * cache.dim
     _check(call(cache, _ptr(K), width if ldk is None else ldk, _ptr(V), width if ldv is None else ldv, _dtype(K, dtype), _ptr(table),
                 _ldt(table, ldt), _ptr(lens), _ptr(cu), batch, M, max_new, max_len, _stream(stream)))
@@ -499,6 +512,7 @@ def cache_attention_workspace_bytes(*, M, heads, kv_heads, dim, batch, max_new, 
 
 def bwta_cache_attention(cache, Q, out, lse, table, lens, cu=None, workspace=None, *, M, batch, max_new, max_len, heads, alpha, causal=True, window=0,
                          ldq=None, ldo=None, ldt=None, dtype=None, workspace_bytes=None, stream=None):
+    _here(cache, Q, out, lse, table, lens, cu, workspace)
     width = heads * cache.dim
     _check(_lib.bwta_cache_attention(cache, _ptr(Q), width if ldq is None else ldq, _ptr(out), width if ldo is None else ldo, _dtype(Q, dtype),
                                      _ptr(lse), _ptr(table), _ldt(table, ldt), _ptr(lens), _ptr(cu), batch, M, max_new, max_len, heads, alpha,
@@ -517,7 +531,7 @@ def _load_native():
         loader.exec_module(module)
     except ImportError as e:  # no such file, or one for another Python or torch
         return None, str(e)
-    module.setup(_check, _raw_stream, _cur_device)
+    module.setup(_check, _raw_stream, _cur_device, Cache)
     return module, module.identity() if hasattr(module, "identity") else "unknown"
 
 
@@ -525,7 +539,7 @@ def _load_native():
 # extension of other sources than the library's (its arguments may be others), or for another torch, is not called.
 _native, _built = _load_native()
 if _built == _native_identity():
-    for _name in _native.parameters():
+    for _name in (*_native.parameters(), *_native.head_parameters()):
         globals()[_name] = _native.bind(_name, _c.cast(getattr(_lib, _name), _P).value, globals()[_name])
 else:
     warnings.warn("%s is of build %r, the library and this interpreter are %r: the calls are marshalled in Python; build again"

@@ -47,6 +47,7 @@ struct Bound {
 };
 
 PyObject *g_check = nullptr, *g_raw_stream = nullptr, *g_device = nullptr;  // binding._check, torch's two stream calls
+PyTypeObject *g_cache = nullptr;                                             // binding.Cache
 
 struct NotOrdinary {};
 
@@ -118,6 +119,66 @@ void *current_stream(PyObject *o)
     }
     return st;
 }
+
+// ---- the operators on heads: tensors of the current device alone, as binding._here has it
+
+struct Here {
+    long device;
+    void *stream;
+    const at::Tensor *tensor(PyObject *o) const
+    {
+        const at::Tensor *t = ::tensor(o);
+        if (t && t->get_device() != device) throw NotOrdinary{};
+        return t;
+    }
+    void *address(PyObject *o) const { return ::address(tensor(o)); }
+};
+
+Here here(PyObject *stream)
+{
+    if (given(stream)) throw NotOrdinary{};
+    PyObject *device = PyObject_CallNoArgs(g_device);
+    PyObject *raw = device ? PyObject_CallOneArg(g_raw_stream, device) : nullptr;
+    Here h{device ? PyLong_AsLong(device) : -1, raw ? PyLong_AsVoidPtr(raw) : nullptr};
+    Py_XDECREF(device);
+    Py_XDECREF(raw);
+    if (PyErr_Occurred()) throw NotOrdinary{};
+    return h;
+}
+
+struct Cache {  // binding.Cache: the C struct, and one more than the number of its tensors' device (0: not known)
+    bwta_cache c;
+    int32_t place;
+};
+
+Cache cache_of(PyObject *o, const Here &h)
+{
+    if (!o || Py_TYPE(o) != g_cache) throw NotOrdinary{};
+    Py_buffer view;
+    if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) != 0) throw NotOrdinary{};
+    Cache c;
+    const bool fits = view.len >= (Py_ssize_t)sizeof c;
+    if (fits) memcpy(&c, view.buf, sizeof c);
+    PyBuffer_Release(&view);
+    if (!fits || (c.place > 0 && c.place - 1 != h.device)) throw NotOrdinary{};
+    return c;
+}
+
+int head_dtype(PyObject *o, const at::Tensor *t)
+{
+    if (given(o)) return int32(o);
+    if (!t || (t->scalar_type() != at::kHalf && t->scalar_type() != at::kBFloat16)) throw NotOrdinary{};
+    return t->scalar_type() == at::kHalf ? BWTA_DTYPE_FP16 : BWTA_DTYPE_BF16;
+}
+
+int flag(PyObject *o, bool otherwise)
+{
+    if (o == nullptr) return otherwise;
+    if (o != Py_True && o != Py_False) throw NotOrdinary{};
+    return o == Py_True;
+}
+
+int64_t rows_apart(PyObject *o, int64_t width) { return given(o) ? int64(o) : width; }
 
 // the C call without the interpreter lock (a launch waits where the queue is full), its code turned into what the Python
 // form returns or raises
@@ -301,6 +362,71 @@ bool matmul_bool_prepared(const Bound &b, PyObject *const *v, PyObject **result)
     return finish([&] { return call((const uint32_t *)pma, strideA, pp, bytes, fmt, batch, M, N, K, pa, am, pb, bm, alpha, po, ldo, stride_out, st); }, result);
 }
 
+bool head_norm_rope(const Bound &b, PyObject *const *v, PyObject **result)
+{
+    const Here h = here(v[21]);
+    const at::Tensor *Q = h.tensor(v[0]), *K = h.tensor(v[1]);
+    const int M = int32(v[8]), heads = int32(v[9]), kv = int32(v[10]), dim = int32(v[11]), rot = (int)rows_apart(v[12], dim);
+    if (given(v[12])) int32(v[12]);
+    const float eps = number(v[13], 1e-6f);
+    const int norm = flag(v[14], true), interleaved = flag(v[15], false);
+    const int64_t wq = (int64_t)heads * dim, wk = (int64_t)kv * dim;
+    const int64_t ldq = rows_apart(v[16], wq), ldk = rows_apart(v[17], wk), ldqo = rows_apart(v[18], wq), ldko = rows_apart(v[19], wk);
+    const int dtype = head_dtype(v[20], Q ? Q : K);
+    void *const pq = address(Q), *const pk = address(K), *const pwq = h.address(v[2]), *const pwk = h.address(v[3]), *const pos = h.address(v[4]),
+               *const freq = h.address(v[5]), *const qo = h.address(v[6]), *const ko = h.address(v[7]);
+    BWTA_FN(bwta_head_norm_rope);
+    return finish([&] { return call(pq, ldq, heads, pwq, pk, ldk, kv, pwk, dtype, M, dim, norm, eps, (const int32_t *)pos, (const float *)freq, rot, interleaved, qo, ldqo, ko, ldko, h.stream); }, result);
+}
+
+template <typename F>
+bool cache_rows(F *call, PyObject *const *v, PyObject **result)
+{
+    const Here h = here(v[14]);
+    const Cache cache = cache_of(v[0], h);
+    const at::Tensor *K = h.tensor(v[1]), *table = h.tensor(v[3]);
+    const int M = int32(v[6]), batch = int32(v[7]), max_new = int32(v[8]), max_len = int32(v[9]);
+    const int64_t width = (int64_t)cache.c.kv_heads * cache.c.dim, ldk = rows_apart(v[10], width), ldv = rows_apart(v[11], width);
+    if (!given(v[12]) && (!table || table->dim() == 0)) throw NotOrdinary{};
+    const int64_t ldt = rows_apart(v[12], table ? table->stride(0) : 0);
+    const int dtype = head_dtype(v[13], K);
+    void *const pk = address(K), *const pv = h.address(v[2]), *const pt = address(table), *const lens = h.address(v[4]), *const cu = h.address(v[5]);
+    return finish([&] { return call(&cache.c, pk, ldk, pv, ldv, dtype, (const int32_t *)pt, ldt, (const int32_t *)lens, (const int32_t *)cu, batch, M, max_new, max_len, h.stream); }, result);
+}
+
+bool cache_write(const Bound &b, PyObject *const *v, PyObject **result)
+{
+    BWTA_FN(bwta_cache_write);
+    return cache_rows(call, v, result);
+}
+
+bool cache_read(const Bound &b, PyObject *const *v, PyObject **result)
+{
+    BWTA_FN(bwta_cache_read);
+    return cache_rows(call, v, result);
+}
+
+bool cache_attention(const Bound &b, PyObject *const *v, PyObject **result)
+{
+    const Here h = here(v[21]);
+    const Cache cache = cache_of(v[0], h);
+    const at::Tensor *Q = h.tensor(v[1]), *table = h.tensor(v[4]), *ws = h.tensor(v[7]);
+    const int M = int32(v[8]), batch = int32(v[9]), max_new = int32(v[10]), max_len = int32(v[11]), heads = int32(v[12]);
+    if (!v[13]) throw NotOrdinary{};
+    const float alpha = number(v[13], 0.0f);
+    const int causal = flag(v[14], true), window = v[15] ? int32(v[15]) : 0;
+    const int64_t width = (int64_t)heads * cache.c.dim, ldq = rows_apart(v[16], width), ldo = rows_apart(v[17], width);
+    if (!given(v[18]) && (!table || table->dim() == 0)) throw NotOrdinary{};
+    const int64_t ldt = rows_apart(v[18], table ? table->stride(0) : 0);
+    const int dtype = head_dtype(v[19], Q);
+    const size_t bytes = bytes_of(v[20], ws);
+    void *const pq = address(Q), *const po = h.address(v[2]), *const lse = h.address(v[3]), *const pt = address(table), *const lens = h.address(v[5]),
+               *const cu = h.address(v[6]), *const pws = address(ws);
+    BWTA_FN(bwta_cache_attention);
+    return finish([&] { return call(&cache.c, pq, ldq, po, ldo, dtype, (float *)lse, (const int32_t *)pt, ldt, (const int32_t *)lens, (const int32_t *)cu, batch, M, max_new, max_len,
+                                    heads, alpha, causal, window, pws, bytes, h.stream); }, result);
+}
+
 const Spec kSpecs[] = {
     {"bwta_linear", 6, {"A", "s_a", "wsign", "s_w", "out", "workspace", "M", "N", "K", "lda", "ldo", "a_scale_mode", "w_scale_mode", "workspace_bytes", "stream"}, linear},
     {"bwta_gemm", 8, {"mask", "sign", "wsign", "s_a", "s_w", "acc", "out", "workspace", "M", "N", "K", "ldo", "a_scale_mode", "w_scale_mode", "workspace_bytes", "stream"}, gemm},
@@ -314,6 +440,18 @@ const Spec kSpecs[] = {
     {"bwta_matmul_tt", 8, {"maskA", "signA", "maskB", "signB", "s_a", "s_b", "acc", "out", "batch", "M", "N", "K", "alpha", "strideA", "strideB", "ldo", "stride_out", "a_scale_mode", "b_scale_mode", "stream"}, matmul_tt},
     {"bwta_matmul_bool_prepared", 5, {"maskA", "preparedB", "s_a", "s_b", "out", "fmt", "batch", "M", "N", "K", "alpha", "strideA", "ldo", "stride_out", "a_scale_mode", "b_scale_mode", "prepared_bytes", "stream"}, matmul_bool_prepared},
 };
+
+const Spec kHeadSpecs[] = {
+    {"bwta_head_norm_rope", 8, {"Q", "K", "wq", "wk", "positions", "inv_freq", "Qout", "Kout", "M", "heads", "kv_heads", "dim", "rot_dim", "eps", "norm", "interleaved", "ldq", "ldk", "ldqo", "ldko", "dtype", "stream"}, head_norm_rope},
+    {"bwta_cache_write", 6, {"cache", "K", "V", "table", "lens", "cu", "M", "batch", "max_new", "max_len", "ldk", "ldv", "ldt", "dtype", "stream"}, cache_write},
+    {"bwta_cache_read", 6, {"cache", "K", "V", "table", "lens", "cu", "M", "batch", "max_new", "max_len", "ldk", "ldv", "ldt", "dtype", "stream"}, cache_read},
+    {"bwta_cache_attention", 8, {"cache", "Q", "out", "lse", "table", "lens", "cu", "workspace", "M", "batch", "max_new", "max_len", "heads", "alpha", "causal", "window", "ldq", "ldo", "ldt", "dtype", "workspace_bytes", "stream"}, cache_attention},
+};
+
+constexpr int kSpecCount = sizeof kSpecs / sizeof kSpecs[0], kHeadSpecCount = sizeof kHeadSpecs / sizeof kHeadSpecs[0];
+
+// positional parameters that may be left out
+bool may_be_left_out(const char *name) { return strcmp(name, "nnz") == 0 || strcmp(name, "cu") == 0 || strcmp(name, "workspace") == 0; }
 
 // the arguments to their parameters' slots; false where the Python form would raise or this table does not know better
 bool place(const Bound &b, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames, PyObject **v)
@@ -330,9 +468,9 @@ bool place(const Bound &b, PyObject *const *args, Py_ssize_t nargs, PyObject *kw
         if (i == b.count || v[at]) return false;
         v[at] = args[nargs + k];
     }
-    // the tensors all have to be given, except nnz, which may be left out
+    // the tensors all have to be given, except some (bwta_linear's and bwta_gemm's workspace are not among them)
     for (int i = 0; i < b.spec->positional; ++i)
-        if (!v[i] && strcmp(b.spec->params[i], "nnz") != 0) return false;
+        if (!v[i] && (i < b.spec->positional - 2 || !may_be_left_out(b.spec->params[i]) || (strcmp(b.spec->params[i], "workspace") == 0 && b.spec->marshal != cache_attention))) return false;
     return true;
 }
 
@@ -397,7 +535,8 @@ PyObject *bind(PyObject *, PyObject *args)
     const char *name;
     PyObject *addr, *fallback;
     if (!PyArg_ParseTuple(args, "sOO", &name, &addr, &fallback)) return nullptr;
-    for (const Spec &s : kSpecs) {
+    for (int n = 0; n < kSpecCount + kHeadSpecCount; ++n) {
+        const Spec &s = n < kSpecCount ? kSpecs[n] : kHeadSpecs[n - kSpecCount];
         if (strcmp(s.name, name) != 0) continue;
         void *const address = PyLong_AsVoidPtr(addr);
         if (PyErr_Occurred()) return nullptr;
@@ -418,20 +557,21 @@ PyObject *bind(PyObject *, PyObject *args)
     return nullptr;
 }
 
-PyObject *setup(PyObject *, PyObject *args)  // (check, raw_stream, device)
+PyObject *setup(PyObject *, PyObject *args)  // (check, raw_stream, device, cache type)
 {
-    PyObject *c, *r, *d;
-    if (!PyArg_ParseTuple(args, "OOO", &c, &r, &d)) return nullptr;
-    Py_INCREF(c), Py_INCREF(r), Py_INCREF(d);
-    Py_XDECREF(g_check), Py_XDECREF(g_raw_stream), Py_XDECREF(g_device);
-    g_check = c, g_raw_stream = r, g_device = d;
+    PyObject *c, *r, *d, *t;
+    if (!PyArg_ParseTuple(args, "OOOO!", &c, &r, &d, &PyType_Type, &t)) return nullptr;
+    Py_INCREF(c), Py_INCREF(r), Py_INCREF(d), Py_INCREF(t);
+    Py_XDECREF(g_check), Py_XDECREF(g_raw_stream), Py_XDECREF(g_device), Py_XDECREF(g_cache);
+    g_check = c, g_raw_stream = r, g_device = d, g_cache = (PyTypeObject *)t;
     Py_RETURN_NONE;
 }
 
-PyObject *parameters(PyObject *, PyObject *)  // {name: (positional parameters, all parameters)}
+PyObject *table_of(const Spec *specs, int count)  // {name: (positional parameters, all parameters)}
 {
     PyObject *out = PyDict_New();
-    for (const Spec &s : kSpecs) {
+    for (int n = 0; n < count; ++n) {
+        const Spec &s = specs[n];
         PyObject *l = out ? PyList_New(0) : nullptr;
         if (!l) break;
         for (int i = 0; s.params[i]; ++i) {
@@ -450,6 +590,9 @@ PyObject *parameters(PyObject *, PyObject *)  // {name: (positional parameters, 
     return out;
 }
 
+PyObject *parameters(PyObject *, PyObject *) { return table_of(kSpecs, kSpecCount); }
+PyObject *head_parameters(PyObject *, PyObject *) { return table_of(kHeadSpecs, kHeadSpecCount); }
+
 #ifndef BWTA_IDENTITY
 #define BWTA_IDENTITY "unknown"
 #endif
@@ -457,7 +600,8 @@ PyObject *identity(PyObject *, PyObject *) { return PyUnicode_FromString(BWTA_ID
 
 PyMethodDef kMethods[] = {{"identity", identity, METH_NOARGS, "identity() -> \"<digest of the sources> <torch version> <Python version>\""},
                           {"bind", bind, METH_VARARGS, "bind(name, address, fallback) -> function"},
-                          {"setup", setup, METH_VARARGS, "setup(check, raw_stream, device)"},
+                          {"setup", setup, METH_VARARGS, "setup(check, raw_stream, device, cache type)"},
+                          {"head_parameters", head_parameters, METH_NOARGS, "as parameters(), of the operators on heads"},
                           {"parameters", parameters, METH_NOARGS, "{name: (positional parameters, all parameters)}"},
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_bwta_native", "Marshalling of the per-layer calls.", -1, kMethods};

@@ -116,6 +116,11 @@ __device__ __forceinline__ void give(const CacheAttentionArgs &a, const Seq &s, 
     if (once && a.lse) a.lse[token * a.heads + h] = kLn2 * (m + log2f(l));
 }
 
+// Workgroups that share `total` steps, as a power of two: not more than there are, so that everybody has one; and where the
+// w-th one's begin.
+__device__ __forceinline__ int shares_log2(const CacheAttentionArgs &a, int total) { return total > 0 ? min(a.share_log2, 31 - __builtin_clz(total)) : 0; }
+__device__ __forceinline__ int share_begin(unsigned w, int total, int log2) { return (int)((uint64_t)w * (unsigned)total >> log2); }
+
 // units of all sequences before each, behind the parts
 __device__ __forceinline__ int *shares_of(const CacheAttentionArgs &a) { return (int *)(a.partial + a.part_rows * (a.cache.dim + 2)); }
 
@@ -163,8 +168,8 @@ __global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_c
             }
         }
         const int before = upto - mine, all = __builtin_amdgcn_readlane(upto, min(63, (a.seq.batch - 1) / each));
-        const uint64_t total = (uint64_t)all * H;  // below 2^31: the host's bound
-        const int u0 = (int)(blockIdx.x * total >> a.share_log2), u1 = (int)((blockIdx.x + 1) * total >> a.share_log2);
+        const int total = all * H, share_log2 = shares_log2(a, total);  // below 2^31: the host's bound
+        const int u0 = share_begin(blockIdx.x, total, share_log2), u1 = share_begin(blockIdx.x + 1, total, share_log2);
         if (blockIdx.x == 0 && wave == 0) {  // for those who join the parts
             int *const table = shares_of(a);
             for (int s = b0, at = before; s < b1; ++s) {
@@ -173,10 +178,11 @@ __global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_c
             }
             if (lane == 0) table[a.seq.batch] = all;
         }
-        if (u0 >= u1) return;
+        if (blockIdx.x >> share_log2 || total == 0) return;
         const int owner = __builtin_ctzll(__ballot(u0 < upto * H));  // the first lane whose sequences reach so far
         int at = __builtin_amdgcn_readlane(before, owner);
         for (b = owner * each;; ++b, at += see.units) {
+            if (b >= a.seq.batch) return;  // only if the lengths change meanwhile
             look_at(b);
             if (u0 < (at + see.units) * H) break;
         }
@@ -385,8 +391,10 @@ __global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_c
         off = 0;  // another workgroup's share ends inside a head's steps, this one's goes on with the next
         if (++head == H) {
             head = 0;
-            do look_at(++b);
-            while (see.units == 0);
+            do {
+                if (++b >= a.seq.batch) return;  // as above
+                look_at(b);
+            } while (see.units == 0);
         }
         __syncthreads();  // before the next part's sums
     }
@@ -700,12 +708,11 @@ __global__ __launch_bounds__(256) void k_cache_attention_join(CacheAttentionArgs
     int64_t second = first + stride;
     int parts = a.splits;
     if (shared) {
-        const int u = units_before * H + h / group * units;
-        const uint64_t total = (uint64_t)units_all * H;
-        auto owner = [&](int x) {  // the workgroup whose share holds unit x; the quotient is at most one off
-            int w = (int)(((double)x + 0.5) * (double)(1 << a.share_log2) / (double)total);
-            if ((int)((uint64_t)w * total >> a.share_log2) > x) --w;
-            if ((int)((uint64_t)(w + 1) * total >> a.share_log2) <= x) ++w;
+        const int u = units_before * H + h / group * units, total = units_all * H, log2 = shares_log2(a, total);
+        auto owner = [&](int x) {  // the workgroup whose share holds step x; the quotient is at most one off
+            int w = (int)(((double)x + 0.5) * (double)(1 << log2) / (double)total);
+            if (share_begin(w, total, log2) > x) --w;
+            if (share_begin(w + 1, total, log2) <= x) ++w;
             return w;
         };
         const int w0 = owner(u), w1 = owner(u + units - 1);

@@ -35,6 +35,9 @@ def run(ref, cache, Q, table, lens, new, heads, alpha, causal, window, rows=None
     M, dim = Q.shape[0], ref.sizes[3]
     cu = np.concatenate(([0], np.cumsum(new))) if cu is None else cu
     seq = dict(M=M, batch=len(lens), max_new=max(max(new), 1) if max_new is None else max_new, max_len=max(lens) if max_len is None else max_len)
+    wide = -(-seq["max_len"] // ref.sizes[2])
+    if table.shape[1] < wide:  # what lies behind a sequence's blocks is not looked at
+        table = torch.cat([table, torch.full((table.shape[0], wide - table.shape[1]), 1 << 30, dtype=torch.int32)], dim=1)
     out = torch.full((M, heads, dim), 33.0, dtype=Q.dtype, device=DEV)
     lse = torch.full((M, heads), 33.0, device=DEV)
     n = B.cache_attention_workspace_bytes(heads=heads, kv_heads=ref.sizes[1], dim=dim, **seq)
@@ -101,6 +104,50 @@ def test_single_tokens(lens, new, heads, kv, block, dim, dtype):
 ])
 def test_several_tokens(lens, new, heads, kv, block, dim, dtype, causal, window):
     case(len(lens) + heads + dim, lens, new, heads, kv, block, dim, dtype, causal, window)
+
+
+@pytest.mark.parametrize("max_len,dim,dtype", [(9000, 128, f16), (131072, 64, b16), (70000, 256, f16)])
+def test_fewer_steps_than_parts(max_len, dim, dtype):
+    """The host's bound is far above the lengths: most of a sequence's parts are empty."""
+    case(31, [10, 70, 0, 640], [1, 1, 0, 1], 4, 2, 64, dim, dtype, max_len=max_len)
+    case(32, [300], [8], 4, 1, 64, dim, dtype, max_len=max_len)
+
+
+@pytest.mark.parametrize("batch,kv,group,dim,dtype,window", [(300, 2, 2, 128, f16, 0), (64, 8, 3, 64, b16, 0), (130, 4, 20, 128, f16, 0), (515, 1, 1, 256, b16, 0), (300, 2, 4, 64, f16, 40)])
+def test_equal_shares_of_ragged_batches(batch, kv, group, dim, dtype, window):
+    """So many sequences of any length, one of them far longer than the others, that workgroups share all steps: shares begin and
+    end inside a head's steps, hold several heads and sequences, and pass over empty ones."""
+    g = torch.Generator().manual_seed(batch)
+    lens = [int(torch.randint(0, 20, (1,), generator=g)) * int(torch.randint(0, 3, (1,), generator=g)) for _ in range(batch)]
+    lens[batch // 3], lens[batch - 2] = 1500, 200
+    new = [min(n, int(torch.randint(0, 3, (1,), generator=g)) // 2 + 1) if n else 0 for n in lens]
+    new = [min(n, 1) for n in new] if group > 16 else new
+    case(batch, lens, new, kv * group, kv, 64, dim, dtype, True, window, max_new=1 if group > 16 else 2, max_len=20000)
+
+
+def test_sequences_without_rows():
+    """Rows that belong to no sequence, in each way the work is laid out."""
+    for batch, kv, max_new, max_len in ((3, 2, 1, 300), (3, 2, 1, 20000), (300, 2, 1, 20000), (3, 2, 50, 300), (2, 1, 50, 20000)):
+        g = torch.Generator().manual_seed(batch)
+        lens = [90] * batch
+        ref, table = filled(g, lens, kv, 64, 64)
+        Q = torch.randn((4, 2 * kv, 64), generator=g).half()
+        got = run(ref, ref.device(B), Q, table, lens, [0] * batch, 2 * kv, 0.1, True, 0, max_new=max_new, max_len=max_len)
+        assert (got[0] == 33).all() and (got[1] == 33).all()
+
+
+@pytest.mark.parametrize("lens,new,heads,kv,dim,dtype,causal,max_len", [
+    ([1100], [100], 2, 1, 128, f16, True, 1100),      # rows held twice, one workgroup's wavefronts in turn
+    ([1100, 60], [90, 60], 3, 1, 64, b16, True, 1100),
+    ([1000, 1090], [70, 33], 2, 2, 128, b16, False, 1100),
+    ([1100, 130], [100, 129], 2, 1, 128, f16, True, 9000),    # eight parts of each row
+    ([1100, 130], [100, 40], 2, 1, 256, b16, True, 5000),
+    ([900], [150], 1, 1, 64, f16, True, 40000),        # many parts of each row
+])
+def test_many_rows_of_long_sequences(lens, new, heads, kv, dim, dtype, causal, max_len):
+    case(len(lens) + dim + max_len, lens, new, heads, kv, 64, dim, dtype, causal, max_len=max_len)
+    if causal:
+        case(7 + len(lens) + dim + max_len, lens, new, heads, kv, 128, dim, dtype, causal, 333, max_len=max_len)
 
 
 @pytest.mark.parametrize("new", [1, 40])
@@ -217,17 +264,18 @@ def test_a_cache_beyond_32_bit_offsets():
         check(ref, Q, small, [400], [new], heads, 0.088, True, 0, got)
 
 
-def _step(cache, s, heads, kv, dim, lens, ws, outs):
+def _step(cache, s, heads, kv, dim, lens, ws, outs, max_len):
     """One decode step of a batch: rotate, write, attend."""
     q, k, v, wq, wk, inv, table = s
     batch = q.shape[0]
-    seq = dict(M=batch, batch=batch, max_new=1, max_len=320)
+    seq = dict(M=batch, batch=batch, max_new=1, max_len=max_len)
     B.bwta_head_norm_rope(q, k, wq, wk, lens - 1, inv, outs[0], outs[1], M=batch, heads=heads, kv_heads=kv, dim=dim)
     B.bwta_cache_write(cache, outs[1], v, table, lens, **seq)
     B.bwta_cache_attention(cache, outs[0], outs[2], outs[3], table, lens, None, ws, heads=heads, alpha=dim ** -0.5, **seq)
 
 
-def test_a_captured_step_replayed_follows_the_lengths():
+@pytest.mark.parametrize("max_len", [320, 20000, 200000])  # a workgroup for each head, parts of each, shares of all
+def test_a_captured_step_replayed_follows_the_lengths(max_len):
     """Rotation, write and attention as one graph, replayed while the lengths grow on the device, against eager steps; then
     both caches hold the same."""
     batch, heads, kv, dim, block = 3, 8, 2, 128, 64
@@ -235,23 +283,23 @@ def test_a_captured_step_replayed_follows_the_lengths():
     lens0 = [120, 1, 255]
     ref, table = filled(g, [320] * 3, kv, block, dim)
     caches = [ref.device(B) for _ in range(2)]
-    table = table.to(DEV)
+    table = torch.cat([table, torch.full((batch, -(-max_len // block) - table.shape[1]), -1, dtype=torch.int32)], dim=1).to(DEV)
     q, k, v = (torch.zeros((batch, n, dim), dtype=f16, device=DEV) for n in (heads, kv, kv))
     wq, wk = (torch.rand(dim, generator=g).half().to(DEV) + 0.5 for _ in range(2))
     inv = (10000.0 ** (-torch.arange(0, dim, 2).double() / dim)).float().to(DEV)
     s = (q, k, v, wq, wk, inv, table)
-    seq = dict(M=batch, batch=batch, max_new=1, max_len=320)
+    seq = dict(M=batch, batch=batch, max_new=1, max_len=max_len)
     n = B.cache_attention_workspace_bytes(heads=heads, kv_heads=kv, dim=dim, **seq)
     wss = [torch.empty(max(n, 256), dtype=torch.uint8, device=DEV) for _ in range(2)]
     outs = [[torch.zeros((batch, m, dim), dtype=f16, device=DEV) for m in (heads, kv, heads)] + [torch.zeros((batch, heads), device=DEV)] for _ in range(2)]
     lens = i32(lens0)
-    _step(caches[0], s, heads, kv, dim, lens, wss[0], outs[0])  # outside the capture once
+    _step(caches[0], s, heads, kv, dim, lens, wss[0], outs[0], max_len)  # outside the capture once
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         lens += 1
-        _step(caches[0], s, heads, kv, dim, lens, wss[0], outs[0])
-    _step(caches[1], s, heads, kv, dim, i32(lens0), wss[1], outs[1])
+        _step(caches[0], s, heads, kv, dim, lens, wss[0], outs[0], max_len)
+    _step(caches[1], s, heads, kv, dim, i32(lens0), wss[1], outs[1], max_len)
     for t in range(1, 6):
         for x in (q, k, v):
             x.copy_(torch.randn(x.shape, generator=g).half() * 2.0 ** t)
@@ -259,7 +307,7 @@ def test_a_captured_step_replayed_follows_the_lengths():
         torch.cuda.synchronize()
         now = i32([a + t for a in lens0])
         assert torch.equal(lens, now)
-        _step(caches[1], s, heads, kv, dim, now, wss[1], outs[1])
+        _step(caches[1], s, heads, kv, dim, now, wss[1], outs[1], max_len)
         torch.cuda.synchronize()
         for a, b in zip(outs[0], outs[1]):
             assert torch.equal(a, b)

@@ -130,7 +130,7 @@ def test_python_forms_check_types_and_caches():
     s = torch.zeros((3, 2))
     c = B.make_cache(k, v, s, s.clone())
     assert (c.blocks, c.kv_heads, c.block, c.dim) == (3, 2, 64, 128) and c.k == k.data_ptr()
-    assert ctypes.sizeof(B.Cache) == 48
+    assert ctypes.sizeof(B.Cache) >= 48 and B.Cache.place.offset == 48 and c.place == 0  # the C struct comes first; host tensors
     for bad in ((k, k, s, s), (k, v, s[:2], s), (k, v, s, torch.zeros((2, 3)).T), (k[0], v, s, s), (k.transpose(2, 3), v.transpose(2, 3), s, s)):
         with pytest.raises(ValueError):
             B.make_cache(*bad)
@@ -140,3 +140,34 @@ def test_python_forms_check_types_and_caches():
         with pytest.raises(TypeError):
             B.make_cache(*bad)
     assert B.make_cache(P[0], P[1], P[2], P[3], blocks=1, kv_heads=1, block=64, dim=64).dim == 64
+
+
+def test_native_marshalling_knows_the_python_forms():
+    """Each call is marshalled with the Python form's parameters, in its order, and hands it what is not the ordinary form."""
+    import inspect
+    table = B._native.head_parameters()
+    assert set(table) == {"bwta_head_norm_rope", "bwta_cache_write", "bwta_cache_read", "bwta_cache_attention"}
+    for name, (positional, params) in table.items():
+        sig = inspect.signature(getattr(B, name))
+        assert [p.name for p in sig.parameters.values()] == params, name
+        assert sum(p.kind is p.POSITIONAL_OR_KEYWORD for p in sig.parameters.values()) == positional, name
+        seen = []
+        f = B._native.bind(name, 0, lambda *a, **k: seen.append((a, k)))  # no address: it must not be called
+        required = {p.name: 1 for p in sig.parameters.values() if p.kind is p.KEYWORD_ONLY and p.default is p.empty}
+        host = torch.zeros(4)
+        for args, kw in (((host,) * positional, required), ((P[0],) * positional, required), ((), {}), ((None,) * (positional + 1), required),
+                         ((None,) * positional, dict(required, M=1.5)), ((None,) * positional, dict(required, stream=0)), ((None,) * positional, dict(required, nothing=1)),
+                         ((bytes(64),) + (None,) * (positional - 1), required)):
+            f(*args, **kw)
+            assert len(seen) == 1 and all(x is y for x, y in zip(seen[0][0], args)) and seen[0][1] == kw
+            seen.clear()
+
+
+def test_host_tensors_are_refused():
+    x = torch.zeros((3, 4, 64), dtype=torch.float16)
+    with pytest.raises(ValueError):
+        rope(Q=x, dtype=None)
+    with pytest.raises(ValueError):
+        rows(B.bwta_cache_write, K=x, dtype=None)
+    with pytest.raises(ValueError):
+        attend(lens=torch.zeros(2, dtype=torch.int32))
