@@ -26,10 +26,10 @@ __device__ __forceinline__ bool place_of(const CacheRowsArgs &a, int per_sequenc
     i /= a.cache.heads;
     const int nth = i % per_sequence, b = i / per_sequence;
     const Seq s = sequence(a.seq, b);
-    const int begin = max(s.start, 0), ordinal = begin / a.cache.block + nth;
+    const int begin = max(s.start, 0), end = min(s.len, s.start + min(s.n, a.seq.max_new)), ordinal = begin / a.cache.block + nth;
     const int64_t from = (int64_t)ordinal * a.cache.block;
-    if (from >= s.len || s.n <= 0) return false;  // from here on everything is below max_len
-    const int t0 = max(begin, (int)from), t1 = (int)min((int64_t)s.len, from + a.cache.block);
+    if (from >= end || s.n <= 0) return false;  // from here on everything is below max_len
+    const int t0 = max(begin, (int)from), t1 = (int)min((int64_t)end, from + a.cache.block);
     if (t0 >= t1) return false;
     p.page = a.seq.table[b * a.seq.ldt + ordinal];
     page_ok = p.page >= 0 && p.page < a.cache.blocks;
@@ -61,32 +61,43 @@ __device__ __forceinline__ uint4 blend(uint4 old, uint4 fresh, int lo, int hi)
 }
 
 // One workgroup owns a block's codes of one head and side: it finds the scale, divides what is there where the scale grew,
-// and writes the new codes.
-template <typename T, int NT>
+// and writes the new codes.  The tokens stay in registers between the two, J times eight values of one token a thread: all of
+// a block's slots, or (NT = 64, J = 1) one token.
+template <typename T, int D, int NT, int J>
 __global__ __launch_bounds__(NT) void k_cache_write(CacheRowsArgs a, int per_sequence)
 {
-    __shared__ uint32_t tile[NT == 64 ? 1 : kCacheTile * 64];  // codes of 64 tokens, [token][dim / 4]
+    constexpr int C = D / 8;
+    __shared__ uint32_t tile[NT == 64 ? 1 : kCacheTile * (D / 4)];  // codes of 64 tokens, [token][D / 4]
     __shared__ uint32_t top_of[NT / 64];
     Place p;
     bool page_ok;
     if (!place_of(a, per_sequence, p, page_ok) || !page_ok) return;
-    const int D = a.cache.dim, block = a.cache.block, tid = threadIdx.x;
-    const int chunks = D / 8, work = p.count * chunks;
-    const T *x = (const T *)(p.value ? a.v : a.k) + p.row * (p.value ? a.ldv : a.ldk) + (int64_t)p.head * D;
+    const int block = a.cache.block, tid = threadIdx.x;
     const int64_t ldx = p.value ? a.ldv : a.ldk;
+    const T *x = (const T *)(p.value ? a.v : a.k) + p.row * ldx + (int64_t)p.head * D;
     const int64_t unit = (int64_t)p.page * a.cache.heads + p.head;
     uint8_t *codes = (p.value ? a.cache.v : a.cache.k) + unit * block * D;
     float *scale = (p.value ? a.cache.v_scale : a.cache.k_scale) + unit;
 
+    // the j-th eight values of a thread: chunk `c` of slot `slot`
+    const int c = tid % C;
+    auto slot_of = [&](int j) { return NT == 64 ? (tid < C ? p.slot : -1) : (tid + j * NT) / C; };
+    auto is_new = [&](int slot) { return slot >= p.slot && slot < p.slot + p.count; };
+    const float before = p.slot > 0 ? *scale : 0.0f;
+    uint4 in[J];
     uint32_t top = 0;  // magnitude bits of a finite 16-bit value order as the values do
-    for (int i = tid; i < work; i += NT) {
-        const uint4 in = *(const uint4 *)(x + (int64_t)(i / chunks) * ldx + i % chunks * 8);
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        const int slot = slot_of(j);
+        in[j] = is_new(slot) ? load_once(x + (int64_t)(slot - p.slot) * ldx + c * 8) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int j = 0; j < J; ++j)
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            const uint32_t lo = (&in.x)[w] & 0x7fff, hi = ((&in.x)[w] >> 16) & 0x7fff;
+            const uint32_t lo = (&in[j].x)[w] & 0x7fff, hi = ((&in[j].x)[w] >> 16) & 0x7fff;
             top = max(top, max(lo < Half<T>::kInf ? lo : 0u, hi < Half<T>::kInf ? hi : 0u));
         }
-    }
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
     if (NT > 64) {
@@ -97,56 +108,63 @@ __global__ __launch_bounds__(NT) void k_cache_write(CacheRowsArgs a, int per_seq
     }
     int e = scale_exponent(Half<T>::to_float(top));
     if (p.slot > 0) {
-        const int before = exponent_of(*scale);
-        if (e > before) {
-            const float f = pow2(before - e);
+        const int was = exponent_of(before);
+        if (e > was) {
+            const float f = pow2(was - e);
             for (int i = tid; i < block * D / 16; i += NT) {  // the whole block: what lies behind the tokens stays in step with its scale
-                uint4 *c = (uint4 *)codes + i;
-                const uint4 old = *c;
-                *c = make_uint4(scaled_codes(old.x, f), scaled_codes(old.y, f), scaled_codes(old.z, f), scaled_codes(old.w, f));
+                uint4 *old = (uint4 *)codes + i;
+                const uint4 o = *old;
+                *old = make_uint4(scaled_codes(o.x, f), scaled_codes(o.y, f), scaled_codes(o.z, f), scaled_codes(o.w, f));
             }
         } else {
-            e = before;
+            e = was;
         }
     }
     __syncthreads();  // everybody has read the scale, and what was there is written before the tokens beside it are
     if (tid == 0) *scale = pow2(e);
     const float inverse = pow2(-e);
 
-    auto codes_of = [&](int token, int chunk) {
-        const uint4 in = *(const uint4 *)(x + (int64_t)token * ldx + chunk * 8);
+    auto codes_of = [&](const uint4 &v) {
         uint2 r;
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
-            const uint32_t u = (&in.x)[2 * w], v = (&in.x)[2 * w + 1];
-            (&r.x)[w] = to_codes(Half<T>::to_float(u & 0xffff) * inverse, Half<T>::to_float(u >> 16) * inverse,
-                                 Half<T>::to_float(v & 0xffff) * inverse, Half<T>::to_float(v >> 16) * inverse);
+            const uint32_t lo = (&v.x)[2 * w], hi = (&v.x)[2 * w + 1];
+            (&r.x)[w] = to_codes(Half<T>::to_float(lo & 0xffff) * inverse, Half<T>::to_float(lo >> 16) * inverse,
+                                 Half<T>::to_float(hi & 0xffff) * inverse, Half<T>::to_float(hi >> 16) * inverse);
         }
         return r;
     };
     if (!p.value) {
-        for (int i = tid; i < work; i += NT) *(uint2 *)(codes + (int64_t)(p.slot + i / chunks) * D + i % chunks * 8) = codes_of(i / chunks, i % chunks);
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+            if (is_new(slot_of(j))) *(uint2 *)(codes + slot_of(j) * D + c * 8) = codes_of(in[j]);
         return;
     }
     if (NT == 64 || p.count <= kFew) {
-        for (int i = tid; i < work; i += NT) {
-            const uint2 r = codes_of(i / chunks, i % chunks);
-            uint8_t *c = codes + (int64_t)(i % chunks * 8) * block + p.slot + i / chunks;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) c[j * block] = (uint8_t)((j < 4 ? r.x : r.y) >> (8 * (j & 3)));
+        for (int j = 0; j < J; ++j) {
+            if (!is_new(slot_of(j))) continue;
+            const uint2 r = codes_of(in[j]);
+            uint8_t *to = codes + c * 8 * block + slot_of(j);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) to[k * block] = (uint8_t)((k < 4 ? r.x : r.y) >> (8 * (k & 3)));
         }
         return;
     }
-    // Through LDS: four rows of 16 tokens per thread, turned by bytes.
-    for (int base = p.slot / kCacheTile * kCacheTile; base < p.slot + p.count; base += kCacheTile) {
-        const int lo = max(p.slot, base), hi = min(p.slot + p.count, base + kCacheTile);
+    // Through LDS, 64 slots at a time: four rows of 16 tokens per thread, turned by bytes.
+    constexpr int kEach = kCacheTile * C / NT > 0 ? kCacheTile * C / NT : 1;  // a thread's chunks of 64 slots
+#pragma unroll
+    for (int t = 0; t < J / kEach; ++t) {
+        const int base = t * kCacheTile, lo = max(p.slot, base), hi = min(p.slot + p.count, base + kCacheTile);
+        if (lo >= hi) continue;
         __syncthreads();
-        for (int i = tid; i < (hi - lo) * chunks; i += NT) {
-            const int token = lo + i / chunks;
-            *(uint2 *)&tile[(token - base) * (D / 4) + i % chunks * 2] = codes_of(token - p.slot, i % chunks);
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            const int slot = slot_of(t * kEach + k);
+            *(uint2 *)&tile[(slot - base) * (D / 4) + c * 2] = codes_of(in[t * kEach + k]);
         }
         __syncthreads();
-        for (int i = tid; i < D / 4 * 4; i += NT) {  // (quarter of the tile, four rows)
+        for (int i = tid; i < D; i += NT) {  // (quarter of the tile, four rows)
             const int q = i & 3, d4 = i >> 2, first = base + 16 * q;
             if (first + 16 <= lo || first >= hi) continue;
             uint4 rows[4];
@@ -154,15 +172,15 @@ __global__ __launch_bounds__(NT) void k_cache_write(CacheRowsArgs a, int per_seq
             for (int w = 0; w < 4; ++w) {
                 uint32_t r[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) r[j] = tile[(16 * q + 4 * w + j) * (D / 4) + d4];
+                for (int k = 0; k < 4; ++k) r[k] = tile[(16 * q + 4 * w + k) * (D / 4) + d4];
                 transpose_bytes(r);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) (&rows[j].x)[w] = r[j];
+                for (int k = 0; k < 4; ++k) (&rows[k].x)[w] = r[k];
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint4 *c = (uint4 *)(codes + (int64_t)(4 * d4 + j) * block + first);
-                *c = first >= lo && first + 16 <= hi ? rows[j] : blend(*c, rows[j], lo - first, hi - first);
+            for (int k = 0; k < 4; ++k) {
+                uint4 *to = (uint4 *)(codes + (4 * d4 + k) * block + first);
+                *to = first >= lo && first + 16 <= hi ? rows[k] : blend(*to, rows[k], lo - first, hi - first);
             }
         }
     }
@@ -203,7 +221,7 @@ __global__ __launch_bounds__(kThreads) void k_cache_read(CacheRowsArgs a, int pe
     const float s = (p.value ? a.cache.v_scale : a.cache.k_scale)[unit];
     if (!p.value) {
         for (int i = tid; i < p.count * chunks; i += kThreads)
-            *(uint4 *)(x + (int64_t)(i / chunks) * ldx + i % chunks * 8) = values_of<T>(*(const uint2 *)(codes + (int64_t)(p.slot + i / chunks) * D + i % chunks * 8), s);
+            store_once(x + (int64_t)(i / chunks) * ldx + i % chunks * 8, values_of<T>(*(const uint2 *)(codes + (int64_t)(p.slot + i / chunks) * D + i % chunks * 8), s));
         return;
     }
     for (int base = p.slot / kCacheTile * kCacheTile; base < p.slot + p.count; base += kCacheTile) {
@@ -228,9 +246,35 @@ __global__ __launch_bounds__(kThreads) void k_cache_read(CacheRowsArgs a, int pe
         __syncthreads();
         for (int i = tid; i < (hi - lo) * chunks; i += kThreads) {
             const int token = lo + i / chunks;
-            *(uint4 *)(x + (int64_t)(token - p.slot) * ldx + i % chunks * 8) = values_of<T>(*(const uint2 *)&tile[(token - base) * (D / 4) + i % chunks * 2], s);
+            store_once(x + (int64_t)(token - p.slot) * ldx + i % chunks * 8, values_of<T>(*(const uint2 *)&tile[(token - base) * (D / 4) + i % chunks * 2], s));
         }
     }
+}
+
+}  // namespace
+
+namespace {
+
+template <typename T, int D>
+void launch_write(const CacheRowsArgs &a, int per, unsigned groups, hipStream_t st)
+{
+    constexpr int kOf64 = kCacheTile * D / 8 / kThreads;  // a thread's chunks of 64 slots
+    if (a.seq.max_new == 1)  // a wavefront does for one token
+        hipLaunchKernelGGL((k_cache_write<T, D, 64, 1>), dim3(groups), dim3(64), 0, st, a, per);
+    else if (a.cache.block == 64)
+        hipLaunchKernelGGL((k_cache_write<T, D, kThreads, kOf64>), dim3(groups), dim3(kThreads), 0, st, a, per);
+    else if (a.cache.block == 128)
+        hipLaunchKernelGGL((k_cache_write<T, D, kThreads, 2 * kOf64>), dim3(groups), dim3(kThreads), 0, st, a, per);
+    else
+        hipLaunchKernelGGL((k_cache_write<T, D, kThreads, 4 * kOf64>), dim3(groups), dim3(kThreads), 0, st, a, per);
+}
+
+template <typename T>
+void launch_write_type(const CacheRowsArgs &a, int per, unsigned groups, hipStream_t st)
+{
+    if (a.cache.dim == 64) launch_write<T, 64>(a, per, groups, st);
+    else if (a.cache.dim == 128) launch_write<T, 128>(a, per, groups, st);
+    else launch_write<T, 256>(a, per, groups, st);
 }
 
 }  // namespace
@@ -239,14 +283,10 @@ hipError_t launch_cache_write(const CacheRowsArgs &a, hipStream_t st)
 {
     const int per = (int)cache_blocks_reached(a.cache, a.seq);
     const unsigned groups = (unsigned)cache_rows_groups(a.cache, a.seq);
-    auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(groups), dim3(threads), 0, st, a, per); };
-    if (a.seq.max_new == 1) {  // a wavefront does for one token
-        if (a.bf16) go(k_cache_write<__bf16, 64>, 64);
-        else go(k_cache_write<_Float16, 64>, 64);
-    } else {
-        if (a.bf16) go(k_cache_write<__bf16, kThreads>, kThreads);
-        else go(k_cache_write<_Float16, kThreads>, kThreads);
-    }
+    if (a.bf16)
+        launch_write_type<__bf16>(a, per, groups, st);
+    else
+        launch_write_type<_Float16>(a, per, groups, st);
     return hipGetLastError();
 }
 

@@ -23,16 +23,6 @@ typedef __bf16 bf2v __attribute__((ext_vector_type(2)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 
-typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
-
-// what one wavefront reads once: past the caches' replacement order (a batch of 32 sequences of 4096 tokens, 32 key heads: 5.1
-// TB/s without, 6.2 with)
-__device__ __forceinline__ uint4 load_once(const uint8_t *p)
-{
-    const uint4v x = __builtin_nontemporal_load((const uint4v *)p);
-    return make_uint4(x.x, x.y, x.z, x.w);
-}
-
 template <typename T> struct Mma;
 template <> struct Mma<_Float16> {
     typedef half8 Frag;
@@ -208,6 +198,8 @@ __global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_c
             bool ok;
         };
         auto page_of = [&](int step) { return a.seq.table[b * a.seq.ldt + (min(step, to - 1) >> block_shift)]; };
+        // (each code is read by one wavefront once: a batch of 32 sequences of 4096 tokens, 32 key heads, 5.1 TB/s through the
+        // caches' order, 6.2 past it)
         auto fetch = [&](Turn &x, int step) {
             const int sub = step & ((1 << block_shift) - 1);
             int page = __builtin_amdgcn_readfirstlane(x.page);

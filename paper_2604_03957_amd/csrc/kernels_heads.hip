@@ -45,7 +45,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_head_norm_rope(HeadRopeArgs a, 
         const int which = h >= a.heads[0], hh = which ? h - a.heads[0] : h;
         const T *x = (const T *)a.x[which] + m * a.ldx[which] + (int64_t)hh * a.dim;
         uint4 in[2] = {};
-        if (has) in[0] = *(const uint4 *)(x + o0), in[1] = *(const uint4 *)(x + o1);
+        if (has) in[0] = load_once(x + o0), in[1] = load_once(x + o1);
         float f[16];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
