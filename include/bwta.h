@@ -296,8 +296,9 @@ int bwta_prepare_act_autoscale(const void *A, int64_t lda, int M, int K, void *s
  * projection.  Queries, keys and values are 16-bit (dtype BWTA_DTYPE_FP16 or BWTA_DTYPE_BF16), one row
  * per token, a row's heads side by side, `dim` elements each, tokens `ld` elements apart: the rows
  * bwta_linear writes, or a part of them (heads of a fused q/k/v projection).  Rows start at 16-byte
- * aligned addresses and ld is a multiple of 8 (BWTA_ERR_ALIGN).  Computation is in fp32, each result is
- * rounded once to dtype.
+ * aligned addresses and ld is a multiple of 8 (BWTA_ERR_ALIGN).  Up to 16384 heads
+ * and, rotated, 2^25 tokens (BWTA_ERR_TOO_LARGE).
+ * Computation is in fp32, each result is rounded once to dtype.
  */
 
 /*
@@ -345,8 +346,9 @@ typedef struct bwta_cache {
  * the sequence's tokens with them, so row cu[b] + i is token lens[b] - n_b + i, n_b = cu[b + 1] - cu[b].
  *   M        rows of the dense arrays; rows of no sequence are neither read nor written
  *   max_new  at least every n_b: rows behind it are left out;  max_len  at least every lens[b]:
- *            larger ones count as max_len.  Both are the host's bounds for the launch; a captured
- *            graph may be replayed with other lens, cu and table contents inside them.
+ *            larger ones count as max_len; at most 2^28 (BWTA_ERR_TOO_LARGE).  Both are the host's
+ *            bounds for the launch; a captured graph may be replayed with other lens, cu and table
+ *            contents inside them.
  *   table    int32, sequence b's row at table + b * ldt, ldt >= ceil(max_len / block); an entry outside
  *            [0, blocks) is a block that is not there (see the calls).
  * lens, cu and table are device memory, 4-byte aligned.

@@ -593,7 +593,7 @@ static int check_cache_call(const bwta_cache *c, int dtype, const int32_t *table
     if (c->block != 64 && c->block != 128 && c->block != 256) return BWTA_ERR_UNSUPPORTED;
     if (c->dim != 64 && c->dim != 128 && c->dim != 256) return BWTA_ERR_UNSUPPORTED;
     if (c->blocks <= 0 || c->kv_heads <= 0 || batch < 0 || M < 0 || max_new < 0 || max_len < 0) return BWTA_ERR_SHAPE;
-    if (c->kv_heads > kMostHeads || max_len > (1 << 30)) return BWTA_ERR_TOO_LARGE;
+    if (c->kv_heads > kMostHeads || max_len > (1 << 28)) return BWTA_ERR_TOO_LARGE;
     if (!cu && (int64_t)batch * max_new > M) return BWTA_ERR_SHAPE;
     if (ldt < ((int64_t)max_len + c->block - 1) / c->block) return BWTA_ERR_SHAPE;
     if (M == 0 || batch == 0 || max_new == 0) {
@@ -661,6 +661,7 @@ int bwta_cache_attention(const bwta_cache *cache, const void *Q, int64_t ldq, vo
     if (heads <= 0 || heads % cache->kv_heads) return BWTA_ERR_SHAPE;
     if (heads > kMostHeads) return BWTA_ERR_TOO_LARGE;
     if (!(alpha > 0.0f && std::isfinite(alpha)) || window < 0 || (window && !causal)) return BWTA_ERR_UNSUPPORTED;
+    if (window >= max_len) window = 0;  // hides nothing, and differences of positions stay inside 32 bits
     if (none) return BWTA_OK;
     if ((rc = check_rows(Q, ldq, heads, cache->dim)) || (rc = check_rows(out, ldo, heads, cache->dim))) return rc;
     if (lse && !aligned(lse, 4)) return BWTA_ERR_ALIGN;

@@ -7,7 +7,7 @@
 // fp16 has 11 bits to bf16's 8.  Value codes enter without their scale; sums are kept in units of 2^eref, the scale of
 // some block, and the few bits between that and the block at hand go into the weights' exponent.
 //
-// Everything stays in registers.  The first product is computed transposed, keys by queries: its result has a query per
+// The first product is computed transposed, keys by queries: its result has a query per
 // lane and, with the key rows taken in the right order (row 4 i + r of the b-th 16 is token 16 i + 4 b + r), 16 tokens in
 // a row per lane, which is what the second product (values transposed by queries) wants as its operand.  Keys are loaded
 // as 16 codes of a token, values as 16 tokens of a channel, both 16 bytes in a row in the cache's layout.
@@ -114,7 +114,11 @@ __device__ __forceinline__ int share_begin(unsigned w, int total, int log2) { re
 // units of all sequences before each, behind the parts
 __device__ __forceinline__ int *shares_of(const CacheAttentionArgs &a) { return (int *)(a.partial + a.part_rows * (a.cache.dim + 2)); }
 
-// Few rows: a workgroup has all NB * 16, and its wavefronts take turns at the steps of 64 keys.
+// Few rows (decoding): a workgroup has all NB * 16, and its wavefronts take turns at the steps of 64 keys, each with what it
+// needs in registers and nothing in LDS until their sums are joined; 16 rows is what the matrix cores take anyway, so heads that
+// share their keys cost nothing.  Bound by the cache's bytes: 64 sequences of 2048 to 8192 tokens, 32 heads on 8 of 128 (680 MB)
+// take 118 us, 5.7 TB/s, equal ones of 8192 6.4 TB/s; one token over 131072 keys (268 MB) 49.5 us with the join, over 2048 keys
+// of 32 heads (17 MB) 11.2 us, most of it the latency of lengths, table and codes one after the other, and of a second launch.
 template <typename T, int D, int NB, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_cache_attention(CacheAttentionArgs a)
 {
@@ -404,6 +408,11 @@ __device__ __forceinline__ constexpr int padded(int row, int chunk) { return row
 // work that does not wait for each other's.  Keys are therefore fetched one step before values.
 // With GROUPS = 2 a workgroup has the rows twice: one four take the even steps, the other the odd ones, and their sums are
 // joined through LDS.
+// Bound by issue: a step of 32 rows is 1024 cycles of matrix cores beside some 1000 of vector ALU (32 weights a lane with a
+// fused multiply-add, a power, an addition and half a conversion each, and the widening), and 32 KB from LDS a wavefront.
+// 8192 keys for each of 2048 rows, 32 heads of 128: 920 TFLOP/s with two groups and 970 with one, where a large fp16 product
+// reaches 1322; 64 rows a wavefront need more registers than the vector ALU can address and copy sums between the two files at
+// every step (half as fast), codes widened by each wavefront cost it 128 conversions a step for 32 (5 % slower).
 template <typename T, int D, int GROUPS>
 __global__ __launch_bounds__(GROUPS * 256, D <= 128 ? 2 : 1) void k_cache_attention_rows(CacheAttentionArgs a, int row_tiles)
 {

@@ -194,3 +194,47 @@ def test_a_cache_beyond_32_bit_offsets():
     for i, p in enumerate(ids):
         n = min(64, 150 - 64 * i)
         assert same_codes(k[p, :, :n].cpu().numpy(), ref.k[i, :, :n]).all() and same_codes(v[p, :, :, :n].cpu().numpy().transpose(0, 2, 1), ref.v[i, :, :n]).all()
+
+
+@pytest.mark.parametrize("max_new", [1, 40, 70])
+def test_rows_beyond_max_new_are_left_out(max_new):
+    """Written: the first max_new rows, as the tokens that they are; read: only they."""
+    block, dim, heads, lens, new = 64, 64, 2, [200, 130], [max_new + 9, max_new]
+    g = torch.Generator().manual_seed(7)
+    cu = np.concatenate(([0], np.cumsum(new)))
+    M = int(cu[-1])
+    K, V = (some_rows(g, M, heads, dim, torch.float16) for _ in range(2))
+    table = torch.randperm(8, generator=g).reshape(2, 4).to(torch.int32)
+    ref = R.Cache(8, heads, block, dim)
+    before = [max(0, n - m) for n, m in zip(lens, new)]  # what is there before
+    K0, V0 = (some_rows(g, sum(before), heads, dim, torch.float16) for _ in range(2))
+    ref.write(K0.double().numpy(), V0.double().numpy(), table, before, np.concatenate(([0], np.cumsum(before))), 2)
+    cache = ref.device(B)
+    kept = [lens[0] - 9, lens[1]]  # the same tokens as a call of max_new rows each
+    rows = [*range(max_new), *range(max_new + 9, M)]
+    ref.write(K[rows].double().numpy(), V[rows].double().numpy(), table, kept, [0, max_new, 2 * max_new], 2)
+    seq = dict(M=M, batch=2, max_new=max_new, max_len=200)
+    B.bwta_cache_write(cache, K.to(DEV), V.to(DEV), table.to(DEV), i32(lens), i32(cu), **seq)
+    torch.cuda.synchronize()
+    check(ref, cache)
+    kb, vb = (torch.full((M, heads, dim), 9.0, dtype=torch.float16, device=DEV) for _ in range(2))
+    B.bwta_cache_read(cache, kb, vb, table.to(DEV), i32(lens), i32(cu), **seq)
+    kb, vb = kb.cpu(), vb.cpu()
+    k, v, _ = ref.rows(table, 0, kept[0])
+    for back, want in ((kb, k), (vb, v)):
+        assert torch.equal(back[:max_new], torch.from_numpy(want[kept[0] - max_new:]).half())
+        assert (back[max_new:max_new + 9] == 9).all() and (back[max_new + 9:] != 9).any()
+
+
+def test_the_same_bits_twice():
+    g = torch.Generator().manual_seed(8)
+    K, V = (some_rows(g, 300, 2, 128, torch.bfloat16).to(DEV) for _ in range(2))
+    ref = R.Cache(6, 2, 64, 128)
+    caches = [ref.device(B) for _ in range(2)]
+    table, lens = i32([[5, 0, 3, 1, 2]]), i32([300])
+    for cache in caches:
+        B.bwta_cache_write(cache, K, V, table, lens, M=300, batch=1, max_new=300, max_len=300)
+        B.bwta_cache_write(cache, 64 * K[:9], V[:9], table, lens + 9, M=9, batch=1, max_new=9, max_len=309)
+    torch.cuda.synchronize()
+    for a, b in zip(caches[0].tensors, caches[1].tensors):
+        assert torch.equal(a, b)

@@ -392,3 +392,112 @@ def test_two_streams_with_workspaces_of_their_own():
                 got[i].append(attend(i, ws[i]))
     torch.cuda.synchronize()
     assert all(torch.equal(x, want[i]) for i in range(2) for x in got[i])
+
+
+@pytest.mark.parametrize("new,max_len", [([30, 5], 20), ([2, 1], 20), ([40, 9], 9000)])
+def test_windows_beyond_every_length(new, max_len):
+    """Up to the largest 32-bit number, rows of negative position among them: the same bits as without one."""
+    g = torch.Generator().manual_seed(24)
+    lens = [20, 5] if new[0] != 2 else [1, 20]
+    ref, table = filled(g, lens, 1, 64, 64)
+    Q = torch.randn((sum(new), 2, 64), generator=g).half()
+    without = run(ref, ref.device(B), Q, table, lens, new, 2, 0.125, True, 0, max_len=max_len)
+    check(ref, Q, table, lens, new, 2, 0.125, True, 0, without)
+    for window in (20, max_len, 2 ** 31 - 1):
+        got = run(ref, ref.device(B), Q, table, lens, new, 2, 0.125, True, window, max_len=max_len)
+        assert torch.equal(got[0], without[0]) and torch.equal(got[1], without[1])
+
+
+@pytest.mark.parametrize("max_new,max_len", [(1, 200), (3, 200), (1, 9000), (40, 200), (40, 40000)])
+def test_rows_beyond_max_new_are_left_out(max_new, max_len):
+    """They keep what is in them; the rows before them stay the tokens that they are."""
+    g = torch.Generator().manual_seed(25)
+    lens, new, heads, kv, dim = [200, 90, 33], [max_new + 3, max_new, max(max_new - 1, 1)], 4, 2, 64
+    ref, table = filled(g, lens, kv, 64, dim)
+    Q = torch.randn((sum(new), heads, dim), generator=g).half()
+    out, lse, cu = run(ref, ref.device(B), Q, table, lens, new, heads, 0.125, True, 0, max_new=max_new, max_len=max_len)
+    want = R.attention(ref, Q.double().numpy(), table, lens, cu, 3, 0.125, True, 0)
+    tol, _ = R.attention_tolerance(f16, *want)
+    left = torch.zeros(sum(new), dtype=torch.bool)
+    left[max_new:max_new + 3] = True
+    assert (out.cpu()[left] == 33).all() and (lse.cpu()[left] == 33).all()
+    err = np.abs(out.double().cpu().numpy() - want[0])[~left.numpy()]
+    assert (err <= tol[~left.numpy()]).all()
+
+
+@pytest.mark.parametrize("new", [[1, 1], [40, 3]])
+def test_scales_of_blocks_that_nobody_names(new):
+    """A block that is not there has no scale either: whatever memory holds instead changes no bit."""
+    g = torch.Generator().manual_seed(26)
+    lens = [300, 260]
+    ref, table = filled(g, lens, 2, 64, 64)
+    table[0, 1], table[1, 0] = -1, 1 << 30
+    free = [p for p in range(ref.sizes[0]) if p not in table.tolist()[0] + table.tolist()[1]]
+    swap = table.clone()  # block 0 is one of those that nobody names
+    swap[table == 0] = free[0]
+    for x in (ref.k, ref.v, ref.ke, ref.ve):
+        x[free[0]] = x[0]
+    Q = torch.randn((sum(new), 4, 64), generator=g).half()
+    got = []
+    for fill in (1.0, float("nan"), float("inf"), 0.0, 2.0 ** 100):
+        cache = ref.device(B)
+        for i in (2, 3):
+            cache.tensors[i][0] = fill
+        got.append(run(ref, cache, Q, swap, lens, new, 4, 0.125, True, 0))
+    check(ref, Q, swap, lens, new, 4, 0.125, True, 0, got[0])
+    for other in got[1:]:
+        assert torch.equal(other[1], got[0][1])
+        err = R.attention_tolerance(f16, *R.attention(ref, Q.double().numpy(), swap, lens, other[2], 2, 0.125, True, 0))[0]
+        assert (np.abs(other[0].double().cpu().numpy() - got[0][0].double().cpu().numpy()) <= 2 * err).all()
+
+
+@pytest.mark.parametrize("lens,new,heads,kv,dim,max_len", [
+    ([700, 90], [1, 1], 8, 2, 128, 704), ([700, 90], [1, 1], 8, 2, 64, 30000), ([5000], [1], 4, 4, 128, 5000),
+    ([700, 90], [90, 40], 4, 2, 64, 704), ([1500], [60], 2, 1, 128, 9000)])
+def test_the_same_bits_twice(lens, new, heads, kv, dim, max_len):
+    g = torch.Generator().manual_seed(27)
+    ref, table = filled(g, lens, kv, 64, dim)
+    Q = torch.randn((sum(new), heads, dim), generator=g).half()
+    cache = ref.device(B)
+    a, b = (run(ref, cache, Q, table, lens, new, heads, 0.1, True, 0, max_len=max_len) for _ in range(2))
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_two_graphs_in_turn():
+    """Two captured calls of different shapes, each with a workspace of its own, replayed in turn and on two streams; then two
+    that share a workspace, replayed one after the other."""
+    g = torch.Generator().manual_seed(28)
+    ref, table = filled(g, [5000, 3000], 2, 64, 128, spread=1)
+    cache, table, lens = ref.device(B), table.to(DEV), i32([5000, 3000])
+    shapes = [(1, 8), (30, 4)]
+    Q = [torch.randn((2 * n, h, 128), generator=g).half().to(DEV) for n, h in shapes]
+    out = [torch.zeros_like(q) for q in Q]
+    seqs = [dict(M=2 * n, batch=2, max_new=n, max_len=5000) for n, _ in shapes]
+    need = [B.cache_attention_workspace_bytes(heads=h, kv_heads=2, dim=128, **s) for (_, h), s in zip(shapes, seqs)]
+    assert all(need)
+
+    def attend(i, ws):
+        B.bwta_cache_attention(cache, Q[i], out[i], None, table, lens, None, ws, heads=shapes[i][1], alpha=0.088, **seqs[i])
+
+    one = torch.empty(max(need), dtype=torch.uint8, device=DEV)
+    want = []
+    for i in range(2):
+        attend(i, one)
+        torch.cuda.synchronize()
+        want.append(out[i].clone())
+    for wss, apart in (([torch.empty(n, dtype=torch.uint8, device=DEV) for n in need], True), ([one, one], False)):
+        graphs = []
+        for i in range(2):
+            graphs.append(torch.cuda.CUDAGraph())
+            with torch.cuda.graph(graphs[i]):
+                attend(i, wss[i])
+        streams = [torch.cuda.Stream() for _ in range(2)]
+        for _ in range(4):
+            for o in out:
+                o.zero_()
+            torch.cuda.synchronize()
+            for i in range(2):
+                with torch.cuda.stream(streams[i if apart else 0]):
+                    graphs[i].replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(o, w) for o, w in zip(out, want))
