@@ -173,7 +173,7 @@ struct CacheAttentionArgs {
     int splits, share_log2, share_rows;
 };
 struct AttentionPlan {
-    int rows, row_tiles, splits, share_log2;
+    int rows, row_tiles, splits, share_log2, waves;
     double groups;  // workgroups
     int64_t part_rows;
     size_t workspace;  // bytes

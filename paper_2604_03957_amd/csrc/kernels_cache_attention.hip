@@ -12,6 +12,7 @@
 // a row per lane, which is what the second product (values transposed by queries) wants as its operand.  Keys are loaded
 // as 16 codes of a token, values as 16 tokens of a channel, both 16 bytes in a row in the cache's layout.
 #include "bwta_heads.h"
+#include <type_traits>
 
 namespace bwta {
 namespace {
@@ -466,29 +467,29 @@ __global__ __launch_bounds__(GROUPS * 256, D <= 128 ? 2 : 1) void k_cache_attent
     int eref = 0;
     const int block_shift = a.cache.block >> 7;  // 64, 128, 256 tokens: 1, 2, 4 steps
 
-    // Loads run ahead of what waits for them.  Steps behind the last are the last again, so that nothing branches on them.
-    uint4 kc[kUnits], vc[kUnits];
+    // Loads run ahead of what waits for them.  Steps behind the last are the last again, but that nobody sees it, so that
+    // nothing branches on them.
+    typedef uint4 Codes[kUnits];
+    Codes kc, vc;
     struct Step {
         int64_t unit;
         int step;
         float ks, vs;
-        bool ok, none;
+        bool ok;
     };
-    int page_ahead;
     auto page_of = [&](int step) { return a.seq.table[b * a.seq.ldt + (min(step, to - 1) >> block_shift)]; };
-    auto next_step = [&](int step) {  // also asks for the block of the step behind it
+    auto step_at = [&](int step, int page) {
         Step r;
         r.step = min(step, to - 1);
-        r.none = step >= to;
-        const int page = __builtin_amdgcn_readfirstlane(page_ahead);
+        page = __builtin_amdgcn_readfirstlane(page);
         r.ok = page >= 0 && page < a.cache.blocks;
         r.unit = (int64_t)(r.ok ? page : 0) * H + head;
+        r.ok &= step < to;
         r.ks = a.cache.k_scale[r.unit];
         r.vs = a.cache.v_scale[r.unit];
-        page_ahead = page_of(step + GROUPS);
         return r;
     };
-    auto fetch_keys = [&](const Step &n) {
+    auto fetch_keys = [&](const Step &n, Codes &kc) {
         const uint8_t *kp = a.cache.k + (n.unit * a.cache.block + (n.step & ((1 << block_shift) - 1)) * kCacheTile) * D;
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) kc[u] = *(const uint4 *)(kp + 16 * (tid + u * NT));
@@ -501,7 +502,7 @@ __global__ __launch_bounds__(GROUPS * 256, D <= 128 ? 2 : 1) void k_cache_attent
             vc[u] = *(const uint4 *)(vp + (at >> 2) * a.cache.block + 16 * (at & 3));
         }
     };
-    auto stage_keys = [&](int buffer) {
+    auto stage_keys = [&](const Codes &kc, int buffer) {
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
             const int at = tid + u * NT, token = at / KK, c = 2 * (at % KK);
@@ -533,8 +534,8 @@ __global__ __launch_bounds__(GROUPS * 256, D <= 128 ? 2 : 1) void k_cache_attent
 
     float16v now[2], ahead[2];  // scores of this step and of the next
     auto hide = [&](const Step &n) {  // keys that a row does not see
-        if (!n.ok || n.none || (n.step + 1) * kCacheTile > all_end || n.step * kCacheTile < all_begin) {
-            const int key0 = n.step * kCacheTile + 16 * h2, hi = n.ok && !n.none ? see_hi : -1;
+        if (!n.ok || (n.step + 1) * kCacheTile > all_end || n.step * kCacheTile < all_begin) {
+            const int key0 = n.step * kCacheTile + 16 * h2, hi = n.ok ? see_hi : -1;
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -558,15 +559,18 @@ __global__ __launch_bounds__(GROUPS * 256, D <= 128 ? 2 : 1) void k_cache_attent
     };
 
     if (from < to) {
-        page_ahead = page_of(from + side);
-        Step s0 = next_step(from + side);
-        fetch_keys(s0);
-        fetch_values(s0);
-        stage_keys(0);
-        stage_values(s0, 0);
-        Step s1 = next_step(from + side + GROUPS);
-        fetch_keys(s1);
-        stage_keys(1);
+        const int page0 = page_of(from + side), page1 = page_of(from + side + GROUPS);
+        int page2 = page_of(from + side + 2 * GROUPS);
+        Step s0 = step_at(from + side, page0), s1 = step_at(from + side + GROUPS, page1);
+        {
+            Codes first;
+            fetch_keys(s0, first);
+            fetch_values(s0);
+            fetch_keys(s1, kc);
+            stage_keys(first, 0);
+            stage_values(s0, 0);
+            stage_keys(kc, 1);
+        }
         __syncthreads();
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
@@ -576,12 +580,17 @@ __global__ __launch_bounds__(GROUPS * 256, D <= 128 ? 2 : 1) void k_cache_attent
         top = largest();
         eref = __builtin_amdgcn_readfirstlane(exponent_of(s0.vs));
 
-        for (int turn = from; turn < to; turn += GROUPS) {
+        // one step; the last one looks at none behind it
+        auto take = [&](int turn, auto last) {
             const int buffer = (turn - from) / GROUPS & 1, step = turn + side;
             __syncthreads();  // keys of the next step and values of this one are there, and nobody reads what is written below
-            const Step s2 = next_step(step + 2 * GROUPS);
-            fetch_keys(s2);
-            fetch_values(s1);
+            Step s2 = s1;
+            if constexpr (!last.value) {
+                s2 = step_at(step + 2 * GROUPS, page2);
+                page2 = page_of(step + 3 * GROUPS);
+                fetch_keys(s2, kc);
+                fetch_values(s1);
+            }
 
             const float c = fmaxf(a.alpha * kLog2e * s0.ks, 1.17549435e-38f);
             const int ev = __builtin_amdgcn_readfirstlane(exponent_of(s0.vs));
@@ -621,8 +630,10 @@ __global__ __launch_bounds__(GROUPS * 256, D <= 128 ? 2 : 1) void k_cache_attent
             };
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk) {
-                score(buffer ^ 1, 0, kk);
-                score(buffer ^ 1, 1, kk);
+                if constexpr (!last.value) {
+                    score(buffer ^ 1, 0, kk);
+                    score(buffer ^ 1, 1, kk);
+                }
                 if (kk % (KK / 4) == 0) weigh(kk / (KK / 4));
             }
 #pragma unroll
@@ -630,12 +641,17 @@ __global__ __launch_bounds__(GROUPS * 256, D <= 128 ? 2 : 1) void k_cache_attent
 #pragma unroll
                 for (int n = 0; n < DN; ++n) gather(n, t);
             l = fmaf((sum[0] + sum[1]) + (sum[2] + sum[3]), undrift, l);
-            hide(s1);
-            top = largest();
-            stage_keys(buffer);
-            stage_values(s1, buffer ^ 1);
-            s0 = s1, s1 = s2;
-        }
+            if constexpr (!last.value) {
+                hide(s1);
+                top = largest();
+                stage_keys(kc, buffer);
+                stage_values(s1, buffer ^ 1);
+                s0 = s1, s1 = s2;
+            }
+        };
+        int turn = from;
+        for (; turn + GROUPS < to; turn += GROUPS) take(turn, std::false_type{});
+        take(turn, std::true_type{});
     }
 
     // o[n][r]: query q32, channel 32 n + 8 (r / 4) + 4 h2 + r % 4, in units of 2^eref
@@ -783,7 +799,7 @@ constexpr int kAttWaves = 4;
 template <typename T, int D>
 void launch(const CacheAttentionArgs &a, const AttentionPlan &plan, hipStream_t st)
 {
-    constexpr int NB = D < 256 ? 2 : 1;
+    constexpr int NB = D < 256 ? 2 : 1, kTwice = D < 256 ? 2 * kAttWaves : kAttWaves;
     const dim3 grid((unsigned)plan.groups), block(kAttWaves * 64);
     if (plan.rows > 32) {
         // Two workgroups' worth of wavefronts on the same rows halve the way of the rows that see most, which is what few
@@ -796,10 +812,13 @@ void launch(const CacheAttentionArgs &a, const AttentionPlan &plan, hipStream_t 
             hipLaunchKernelGGL((k_cache_attention_rows<T, D, kMost>), grid, dim3(kMost * 256), 0, st, a, plan.row_tiles);
         else
             hipLaunchKernelGGL((k_cache_attention_rows<T, D, 1>), grid, block, 0, st, a, plan.row_tiles);
-    } else if (plan.rows == 16)
-        hipLaunchKernelGGL((k_cache_attention<T, D, 1, kAttWaves>), grid, block, 0, st, a);
-    else
-        hipLaunchKernelGGL((k_cache_attention<T, D, NB, kAttWaves>), grid, block, 0, st, a);
+    } else if (plan.rows == 16) {
+        if (plan.waves == kAttWaves) hipLaunchKernelGGL((k_cache_attention<T, D, 1, kAttWaves>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((k_cache_attention<T, D, 1, kTwice>), grid, dim3(kTwice * 64), 0, st, a);
+    } else {
+        if (plan.waves == kAttWaves) hipLaunchKernelGGL((k_cache_attention<T, D, NB, kAttWaves>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((k_cache_attention<T, D, NB, kTwice>), grid, dim3(kTwice * 64), 0, st, a);
+    }
     if (plan.workspace) {
         const int64_t rows = (int64_t)a.seq.batch * a.seq.max_new * a.heads, alone = 256 / (D / 4);
         if (a.splits > 1 && a.splits <= kFewSplits)
@@ -828,7 +847,7 @@ AttentionPlan cache_attention_plan(int M, int heads, int kv_heads, int dim, int 
     p.rows = rows <= 16 ? 16 : rows <= 32 && dim < 256 ? 32 : 128;
     p.row_tiles = (int)((rows + p.rows - 1) / p.rows);
     p.groups = (double)p.row_tiles * parts;
-    p.splits = 1, p.share_log2 = -1;
+    p.splits = 1, p.share_log2 = -1, p.waves = kAttWaves;
     if (p.rows <= 32) {
         // Two workgroups for every compute unit, as long as each of their wavefronts still has a step: every sequence is split
         // into as many parts, and a long one's take longer, which is little where they are short (us, a token over 131072 keys
@@ -837,7 +856,11 @@ AttentionPlan cache_attention_plan(int M, int heads, int kv_heads, int dim, int 
         const int64_t want = parts >= 512 ? 1 : (int64_t)((512 + parts - 1) / parts), most_splits = steps / kAttWaves;
         const int64_t splits = want < most_splits ? want : most_splits > 1 ? most_splits : 1;
         if (steps <= 8 * kAttWaves * splits || all >= (double)(1u << 31)) {
-            if (splits > 1) {
+            if (splits == 2 && dim < 256) {
+                // twice the wavefronts, which join in LDS (32 sequences of 2048 keys, 8 heads of 128: 24.5 us, two parts 27.6;
+                // 512 keys, one sequence: 7.4 and 8.8); heads of 256 have no registers for that
+                p.waves = 2 * kAttWaves;
+            } else if (splits > 2) {
                 p.splits = (int)splits;
                 p.groups *= (double)splits;
                 p.part_rows = (int64_t)p.groups * p.rows;

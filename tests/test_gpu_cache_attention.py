@@ -501,3 +501,11 @@ def test_two_graphs_in_turn():
                     graphs[i].replay()
             torch.cuda.synchronize()
             assert all(torch.equal(o, w) for o, w in zip(out, want))
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("heads,kv,dtype", [(6, 2, f16), (20, 1, b16), (32, 1, f16)])
+@pytest.mark.parametrize("window", [0, 130])
+def test_sequences_of_eight_to_eleven_steps(dim, heads, kv, dtype, window):
+    """So long that a workgroup of twice the wavefronts has one, a last step that holds one key, one sequence without any."""
+    case(41 + dim + heads, [513, 700, 0, 20], [1, 1, 0, 1], heads, kv, 64, dim, dtype, True, window)
