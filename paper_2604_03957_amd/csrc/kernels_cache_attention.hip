@@ -407,6 +407,27 @@ __device__ __forceinline__ constexpr int padded(int row, int chunk) { return row
 // token 16 j + 4 i + r, so a lane again has 16 tokens in a row.
 // A turn computes the scores of the next step beside the weights and the sums of this one: matrix cores and vector ALU have
 // work that does not wait for each other's.  Keys are therefore fetched one step before values.
+// Workgroups that share all steps equally (share_log2 >= 0) go through those of a sequence's first head's first 128 rows, second
+// 128 and so on, next head, next sequence; what begins or ends inside somebody else's share becomes a part, and each leaves
+// where it begins for the join.
+struct RowsReach {
+    int step0, steps, units;  // as Reach's, of the rows of one tile
+};
+constexpr int kTileRows = 128, kMostShared = 1024;  // tiles that are shared at most (sequences, too: a workgroup counts each one's steps)
+__device__ __forceinline__ RowsReach rows_reach(const CacheAttentionArgs &a, const Seq &s, int group, int total, int tile)
+{
+    const int first = tile * kTileRows, last = min(first + kTileRows, total) - 1;
+    const int t_first = (unsigned)first / (unsigned)group, t_last = (unsigned)last / (unsigned)group;
+    const int end = a.causal ? max(0, min(s.len, s.start + t_last + 1)) : s.len, begin = a.window ? max(0, s.start + t_first - a.window + 1) : 0;
+    RowsReach r;
+    r.step0 = begin / kCacheTile;
+    r.steps = max(0, (end + kCacheTile - 1) / kCacheTile - r.step0);
+    r.units = max(r.steps, 1);
+    return r;
+}
+// where each sharing workgroup begins, behind the parts: sequence (-1: nowhere), head, tile, steps of the tile before it
+__device__ __forceinline__ int4 *begins_of(const CacheAttentionArgs &a) { return (int4 *)(a.partial + a.part_rows * (a.cache.dim + 2)); }
+
 // With GROUPS = 2 a workgroup has the rows twice: one four take the even steps, the other the odd ones, and their sums are
 // joined through LDS.
 // Bound by issue: a step of 32 rows is 1024 cycles of matrix cores beside some 1000 of vector ALU (32 weights a lane with a
@@ -414,10 +435,10 @@ __device__ __forceinline__ constexpr int padded(int row, int chunk) { return row
 // 8192 keys for each of 2048 rows, 32 heads of 128: 920 TFLOP/s with two groups and 970 with one, where a large fp16 product
 // reaches 1322; 64 rows a wavefront need more registers than the vector ALU can address and copy sums between the two files at
 // every step (half as fast), codes widened by each wavefront cost it 128 conversions a step for 32 (5 % slower).
-template <typename T, int D, int GROUPS>
+template <typename T, int D, int GROUPS, bool SHARES>
 __global__ __launch_bounds__(GROUPS * 256, D <= 128 ? 2 : 1) void k_cache_attention_rows(CacheAttentionArgs a, int row_tiles)
 {
-    constexpr int WAVES = 4, R = 32, kRows = R * WAVES, NT = WAVES * 64, KK = D / 16, DN = D / 32, kUnits = 4 * D / NT;
+    constexpr int WAVES = 4, R = 32, kRows = kTileRows, NT = WAVES * 64, KK = D / 16, DN = D / 32, kUnits = 4 * D / NT;
     typedef typename Mma<T>::Frag Frag;
     struct Tile {
         uint4 keys[kCacheTile * (D / 8 + 1)], values[D * (kCacheTile / 8 + 1)];
@@ -427,273 +448,397 @@ __global__ __launch_bounds__(GROUPS * 256, D <= 128 ? 2 : 1) void k_cache_attent
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), q32 = lane & 31, h2 = lane >> 5;
     const int H = a.cache.heads, group = a.heads / H;
 
-    unsigned i = blockIdx.x;
-    const int split = i % a.splits;
-    i /= a.splits;
-    // Causal rows at the end see most: first.  Workgroups go around the eight XCDs, and inside one around its four shader
-    // engines, in order: consecutive ones have the heads of a sequence, and sequences change places from one round of all of
-    // them to the next, or a long one would always fall to the same engines (half of the time of a ragged batch of four).
-    const int round = (int)(i / (a.seq.batch * H)), bh = i % (a.seq.batch * H), head = bh % H, b = (bh / H + round) % a.seq.batch;
-    const int tile_of_rows = row_tiles - 1 - round;
-    const Seq s = sequence(a.seq, b);
-    const int total = min(s.n, a.seq.max_new) * group, first = tile_of_rows * kRows;
-    if (first >= total) return;
-
-    // keys that some row sees, and those that every row of this wavefront sees
-    const int my_first = min(first + wave * R, total - 1), my_last = min(my_first + R, total) - 1, last = min(first + kRows, total) - 1;
-    const int t_first = (unsigned)first / (unsigned)group, t_last = (unsigned)last / (unsigned)group;
-    const int key_end = a.causal ? max(0, min(s.len, s.start + t_last + 1)) : s.len;
-    const int key_begin = a.window ? max(0, s.start + t_first - a.window + 1) : 0;
-    const int all_end = a.causal ? min(s.len, s.start + (int)((unsigned)my_first / (unsigned)group) + 1) : s.len;
-    const int all_begin = a.window ? s.start + (int)((unsigned)my_last / (unsigned)group) - a.window + 1 : 0;
-    const int step0 = key_begin / kCacheTile, steps = max(0, (key_end + kCacheTile - 1) / kCacheTile - step0);
-    const int from = step0 + (unsigned)(steps * split) / (unsigned)a.splits, to = step0 + (unsigned)(steps * (split + 1)) / (unsigned)a.splits;
-
-    // this lane's query
-    const int row = first + wave * R + q32;
-    const bool has = row < total;
-    const int token = has ? (unsigned)row / (unsigned)group : 0;
-    const int see_hi = !has ? -1 : a.causal ? min(s.len - 1, s.start + token) : s.len - 1, see_lo = a.window ? s.start + token - a.window + 1 : 0;
-    Frag q[KK];
-    const T *query = (const T *)a.q + (s.row + token) * a.ldq + (int64_t)(head * group + (has ? row - token * group : 0)) * D + 8 * h2;
+    int b, head, tile_of_rows, off = 0, left = 0;
+    unsigned share = 0;
+    Seq s;
+    if constexpr (!SHARES) {
+        // Causal rows at the end see most: first.  Workgroups go around the eight XCDs, and inside one around its four shader
+        // engines, in order: consecutive ones have the heads of a sequence, and sequences change places from one round of all of
+        // them to the next, or a long one would always fall to the same engines (half of the time of a ragged batch of four).
+        const unsigned i = blockIdx.x / a.splits;
+        const int round = (int)(i / (a.seq.batch * H)), bh = i % (a.seq.batch * H);
+        head = bh % H, b = (bh / H + round) % a.seq.batch;
+        tile_of_rows = row_tiles - 1 - round;
+        s = sequence(a.seq, b);
+        if (tile_of_rows * kRows >= min(s.n, a.seq.max_new) * group) return;
+    } else {
+        // steps of each sequence, for one head
+        int *const steps_of = (int *)&tiles[0][0];
+        static_assert(sizeof(tiles) >= kMostShared * sizeof(int), "the counts go where keys and values will be");
+        for (int i = threadIdx.x; i < a.seq.batch; i += GROUPS * NT) steps_of[i] = 0;
+        __syncthreads();
+        for (int i = threadIdx.x; i < a.seq.batch * row_tiles; i += GROUPS * NT) {
+            const int c = i / row_tiles, tile = i - c * row_tiles;
+            const Seq x = sequence(a.seq, c);
+            const int total = min(x.n, a.seq.max_new) * group;
+            if (tile * kRows < total) atomicAdd(&steps_of[c], rows_reach(a, x, group, total, tile).units);
+        }
+        __syncthreads();
+        const int each = (a.seq.batch + 63) / 64, b0 = min(lane * each, a.seq.batch), b1 = min(b0 + each, a.seq.batch);
+        int mine = 0;
+        for (int c = b0; c < b1; ++c) mine += steps_of[c];
+        int upto = mine;
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-        if (has) q[kk] = *(const Frag *)(query + 16 * kk);
-        else q[kk] = Frag{};
+        for (int d = 1; d < 64; d *= 2) {
+            const int x = __shfl_up(upto, d);
+            if (lane >= d) upto += x;
+        }
+        const int all = __builtin_amdgcn_readlane(upto, 63) * H, share_log2 = shares_log2(a, all);  // below 2^31: the host's bound
+        // an XCD's workgroups (every eighth) have shares in a row, of few heads: their keys and values stay in its L2
+        const unsigned low = blockIdx.x & ((1u << share_log2) - 1);
+        share = share_log2 < 3 ? blockIdx.x : (blockIdx.x - low) | (low & 7) << (share_log2 - 3) | low >> 3;
+        if (share >> share_log2 || all == 0) {
+            if (threadIdx.x == 0) begins_of(a)[share] = make_int4(-1, 0, 0, 0);
+            return;
+        }
+        const int u0 = share_begin(share, all, share_log2);
+        left = share_begin(share + 1, all, share_log2) - u0;
+        const int owner = __builtin_ctzll(__ballot(u0 < upto * H));  // the first lane whose sequences reach so far
+        int at = __builtin_amdgcn_readlane(upto - mine, owner);
+        for (b = owner * each;; ++b) {
+            const int of = __builtin_amdgcn_readfirstlane(steps_of[b]);
+            if (u0 < (at + of) * H) {
+                off = u0 - at * H;
+                head = off / of, off -= head * of;
+                break;
+            }
+            at += of;
+        }
+        s = sequence(a.seq, b);
+        const int total = min(s.n, a.seq.max_new) * group, last_tile = (total - 1) / kRows;
+        for (tile_of_rows = 0;; tile_of_rows += 64) {
+            const int tile = tile_of_rows + lane, units = tile <= last_tile ? rows_reach(a, s, group, total, tile).units : 0;
+            int to = units;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const int x = __shfl_up(to, d);
+                if (lane >= d) to += x;
+            }
+            const uint64_t reached = __ballot(off < to);
+            if (reached || tile_of_rows + 64 > last_tile) {
+                const int l = reached ? __builtin_ctzll(reached) : 0;
+                off -= __builtin_amdgcn_readlane(to - units, l), tile_of_rows += l;
+                break;
+            }
+            off -= __builtin_amdgcn_readlane(to, 63);
+        }
+        if (threadIdx.x == 0) begins_of(a)[share] = make_int4(b, head, tile_of_rows, off);
+        __syncthreads();  // the counts are read
     }
 
-    float16v o[DN] = {};
-    float m = -INFINITY, l = 0.0f, top = -INFINITY;
-    int eref = 0;
-    const int block_shift = a.cache.block >> 7;  // 64, 128, 256 tokens: 1, 2, 4 steps
+    for (;;) {
+        const int total = min(s.n, a.seq.max_new) * group, first = tile_of_rows * kRows;
+        // keys that some row sees, and those that every row of this wavefront sees
+        const RowsReach see = rows_reach(a, s, group, total, tile_of_rows);
+        const int my_first = min(first + wave * R, total - 1), my_last = min(my_first + R, total) - 1;
+        const int all_end = a.causal ? min(s.len, s.start + (int)((unsigned)my_first / (unsigned)group) + 1) : s.len;
+        const int all_begin = a.window ? s.start + (int)((unsigned)my_last / (unsigned)group) - a.window + 1 : 0;
+        int take = see.units, from = see.step0, to = see.step0 + see.steps;
+        int64_t part0 = -1;  // of this tile's rows, if what comes out is a part of them
+        if constexpr (SHARES) {
+            take = max(min(see.units - off, left), 1);
+            from += off, to = min(from + take, to);
+            if (take < see.units) part0 = (2 * (int64_t)share + (off == 0)) * kRows;  // began in another workgroup's share, or ends in one
+        } else if (a.splits > 1) {
+            const int split = blockIdx.x % a.splits;
+            from += (unsigned)(see.steps * split) / (unsigned)a.splits, to = see.step0 + (unsigned)(see.steps * (split + 1)) / (unsigned)a.splits;
+        }
 
-    // Loads run ahead of what waits for them.  Steps behind the last are the last again, but that nobody sees it, so that
-    // nothing branches on them.
-    typedef uint4 Codes[kUnits];
-    Codes kc, vc;
-    struct Step {
-        int64_t unit;
-        int step;
-        float ks, vs;
-        bool ok;
-    };
-    auto page_of = [&](int step) { return a.seq.table[b * a.seq.ldt + (min(step, to - 1) >> block_shift)]; };
-    auto step_at = [&](int step, int page) {
-        Step r;
-        r.step = min(step, to - 1);
-        page = __builtin_amdgcn_readfirstlane(page);
-        r.ok = page >= 0 && page < a.cache.blocks;
-        r.unit = (int64_t)(r.ok ? page : 0) * H + head;
-        r.ok &= step < to;
-        r.ks = a.cache.k_scale[r.unit];
-        r.vs = a.cache.v_scale[r.unit];
-        return r;
-    };
-    auto fetch_keys = [&](const Step &n, Codes &kc) {
-        const uint8_t *kp = a.cache.k + (n.unit * a.cache.block + (n.step & ((1 << block_shift) - 1)) * kCacheTile) * D;
+        // this lane's query
+        const int row = first + wave * R + q32;
+        const bool has = row < total;
+        const int token = has ? (unsigned)row / (unsigned)group : 0;
+        const int see_hi = !has ? -1 : a.causal ? min(s.len - 1, s.start + token) : s.len - 1, see_lo = a.window ? s.start + token - a.window + 1 : 0;
+        Frag q[KK];
+        const T *query = (const T *)a.q + (s.row + token) * a.ldq + (int64_t)(head * group + (has ? row - token * group : 0)) * D + 8 * h2;
 #pragma unroll
-        for (int u = 0; u < kUnits; ++u) kc[u] = *(const uint4 *)(kp + 16 * (tid + u * NT));
-    };
-    auto fetch_values = [&](const Step &n) {
-        const uint8_t *vp = a.cache.v + n.unit * D * a.cache.block + (n.step & ((1 << block_shift) - 1)) * kCacheTile;
-#pragma unroll
-        for (int u = 0; u < kUnits; ++u) {
-            const int at = tid + u * NT;
-            vc[u] = *(const uint4 *)(vp + (at >> 2) * a.cache.block + 16 * (at & 3));
+        for (int kk = 0; kk < KK; ++kk) {
+            if (has) q[kk] = *(const Frag *)(query + 16 * kk);
+            else q[kk] = Frag{};
         }
-    };
-    auto stage_keys = [&](const Codes &kc, int buffer) {
+
+        float16v o[DN] = {};
+        float m = -INFINITY, l = 0.0f, top = -INFINITY;
+        int eref = 0;
+        const int block_shift = a.cache.block >> 7;  // 64, 128, 256 tokens: 1, 2, 4 steps
+
+        // Loads run ahead of what waits for them.  Steps behind the last are the last again, but that nobody sees it, so that
+        // nothing branches on them.
+        typedef uint4 Codes[kUnits];
+        Codes kc, vc;
+        struct Step {
+            int64_t unit;
+            int step;
+            float ks, vs;
+            bool ok;
+        };
+        auto page_of = [&](int step) { return a.seq.table[b * a.seq.ldt + (min(step, to - 1) >> block_shift)]; };
+        auto step_at = [&](int step, int page) {
+            Step r;
+            r.step = min(step, to - 1);
+            page = __builtin_amdgcn_readfirstlane(page);
+            r.ok = page >= 0 && page < a.cache.blocks;
+            r.unit = (int64_t)(r.ok ? page : 0) * H + head;
+            r.ok &= step < to;
+            r.ks = a.cache.k_scale[r.unit];
+            r.vs = a.cache.v_scale[r.unit];
+            return r;
+        };
+        auto fetch_keys = [&](const Step &n, Codes &kc) {
+            const uint8_t *kp = a.cache.k + (n.unit * a.cache.block + (n.step & ((1 << block_shift) - 1)) * kCacheTile) * D;
 #pragma unroll
-        for (int u = 0; u < kUnits; ++u) {
-            const int at = tid + u * NT, token = at / KK, c = 2 * (at % KK);
-            const int row = (token & 32) + 8 * (token >> 2 & 3) + 4 * (token >> 4 & 1) + (token & 3);
-            *(Frag *)&tiles[side][buffer].keys[padded<D / 8>(row, c)] = widen<T>(kc[u].x, kc[u].y);
-            *(Frag *)&tiles[side][buffer].keys[padded<D / 8>(row, c + 1)] = widen<T>(kc[u].z, kc[u].w);
-        }
-    };
-    auto stage_values = [&](const Step &n, int buffer) {
-        // a slot behind the sequence holds anything, a NaN too: its weight 0 does not hide that
-        if (!n.ok || (n.step + 1) * kCacheTile > s.len) {
+            for (int u = 0; u < kUnits; ++u) kc[u] = *(const uint4 *)(kp + 16 * (tid + u * NT));
+        };
+        auto fetch_values = [&](const Step &n) {
+            const uint8_t *vp = a.cache.v + n.unit * D * a.cache.block + (n.step & ((1 << block_shift) - 1)) * kCacheTile;
 #pragma unroll
             for (int u = 0; u < kUnits; ++u) {
-                const int valid = n.ok ? s.len - n.step * kCacheTile - 16 * ((tid + u * NT) & 3) : 0;
+                const int at = tid + u * NT;
+                vc[u] = *(const uint4 *)(vp + (at >> 2) * a.cache.block + 16 * (at & 3));
+            }
+        };
+        auto stage_keys = [&](const Codes &kc, int buffer) {
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const int bytes = min(max(valid - 4 * w, 0), 4);
-                    (&vc[u].x)[w] &= bytes == 4 ? 0xffffffffu : (1u << (8 * bytes)) - 1;
+            for (int u = 0; u < kUnits; ++u) {
+                const int at = tid + u * NT, token = at / KK, c = 2 * (at % KK);
+                const int row = (token & 32) + 8 * (token >> 2 & 3) + 4 * (token >> 4 & 1) + (token & 3);
+                *(Frag *)&tiles[side][buffer].keys[padded<D / 8>(row, c)] = widen<T>(kc[u].x, kc[u].y);
+                *(Frag *)&tiles[side][buffer].keys[padded<D / 8>(row, c + 1)] = widen<T>(kc[u].z, kc[u].w);
+            }
+        };
+        auto stage_values = [&](const Step &n, int buffer) {
+            // a slot behind the sequence holds anything, a NaN too: its weight 0 does not hide that
+            if (!n.ok || (n.step + 1) * kCacheTile > s.len) {
+#pragma unroll
+                for (int u = 0; u < kUnits; ++u) {
+                    const int valid = n.ok ? s.len - n.step * kCacheTile - 16 * ((tid + u * NT) & 3) : 0;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const int bytes = min(max(valid - 4 * w, 0), 4);
+                        (&vc[u].x)[w] &= bytes == 4 ? 0xffffffffu : (1u << (8 * bytes)) - 1;
+                    }
                 }
             }
-        }
 #pragma unroll
-        for (int u = 0; u < kUnits; ++u) {
-            const int at = tid + u * NT, d = at >> 2, c = 2 * (at & 3);
-            *(half8 *)&tiles[side][buffer].values[padded<8>(d, c)] = widen<_Float16>(vc[u].x, vc[u].y);
-            *(half8 *)&tiles[side][buffer].values[padded<8>(d, c + 1)] = widen<_Float16>(vc[u].z, vc[u].w);
-        }
-    };
+            for (int u = 0; u < kUnits; ++u) {
+                const int at = tid + u * NT, d = at >> 2, c = 2 * (at & 3);
+                *(half8 *)&tiles[side][buffer].values[padded<8>(d, c)] = widen<_Float16>(vc[u].x, vc[u].y);
+                *(half8 *)&tiles[side][buffer].values[padded<8>(d, c + 1)] = widen<_Float16>(vc[u].z, vc[u].w);
+            }
+        };
 
-    float16v now[2], ahead[2];  // scores of this step and of the next
-    auto hide = [&](const Step &n) {  // keys that a row does not see
-        if (!n.ok || (n.step + 1) * kCacheTile > all_end || n.step * kCacheTile < all_begin) {
-            const int key0 = n.step * kCacheTile + 16 * h2, hi = n.ok ? see_hi : -1;
+        float16v now[2], ahead[2];  // scores of this step and of the next
+        auto hide = [&](const Step &n) {  // keys that a row does not see
+            if (!n.ok || (n.step + 1) * kCacheTile > all_end || n.step * kCacheTile < all_begin) {
+                const int key0 = n.step * kCacheTile + 16 * h2, hi = n.ok ? see_hi : -1;
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int key = key0 + 32 * kb + r;
+                        ahead[kb][r] = ((key > hi) | (key < see_lo)) ? -INFINITY : ahead[kb][r];
+                    }
+            }
+        };
+        auto largest = [&] {
+            float x = -INFINITY;
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int key = key0 + 32 * kb + r;
-                    ahead[kb][r] = ((key > hi) | (key < see_lo)) ? -INFINITY : ahead[kb][r];
-                }
-        }
-    };
-    auto largest = [&] {
-        float x = -INFINITY;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int r = 0; r < 16; r += 2) x = most(x, most(ahead[kb][r], ahead[kb][r + 1]));
-        return x;
-    };
-    auto score = [&](int buffer, int kb, int kk) {
-        const Frag f = *(const Frag *)&tiles[side][buffer].keys[padded<D / 8>(32 * kb + q32, 2 * kk + h2)];
-        ahead[kb] = Mma<T>::mma(f, q[kk], kk == 0 ? float16v{} : ahead[kb]);
-    };
-
-    if (from < to) {
-        const int page0 = page_of(from + side), page1 = page_of(from + side + GROUPS);
-        int page2 = page_of(from + side + 2 * GROUPS);
-        Step s0 = step_at(from + side, page0), s1 = step_at(from + side + GROUPS, page1);
-        {
-            Codes first;
-            fetch_keys(s0, first);
-            fetch_values(s0);
-            fetch_keys(s1, kc);
-            stage_keys(first, 0);
-            stage_values(s0, 0);
-            stage_keys(kc, 1);
-        }
-        __syncthreads();
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int kk = 0; kk < KK; ++kk) score(0, kb, kk);
-        hide(s0);
-        top = largest();
-        eref = __builtin_amdgcn_readfirstlane(exponent_of(s0.vs));
-
-        // one step; the last one looks at none behind it
-        auto take = [&](int turn, auto last) {
-            const int buffer = (turn - from) / GROUPS & 1, step = turn + side;
-            __syncthreads();  // keys of the next step and values of this one are there, and nobody reads what is written below
-            Step s2 = s1;
-            if constexpr (!last.value) {
-                s2 = step_at(step + 2 * GROUPS, page2);
-                page2 = page_of(step + 3 * GROUPS);
-                fetch_keys(s2, kc);
-                fetch_values(s1);
-            }
-
-            const float c = fmaxf(a.alpha * kLog2e * s0.ks, 1.17549435e-38f);
-            const int ev = __builtin_amdgcn_readfirstlane(exponent_of(s0.vs));
-            if (ev - eref > kDrift || eref - ev > kDrift) {
-                const float f = pow2(eref - ev);
-                eref = ev;
-#pragma unroll
-                for (int n = 0; n < DN; ++n) o[n] *= f;
-            }
-            const float drift = (float)(ev - eref), undrift = pow2(eref - ev);
-            top *= c;
-            if (__any(top > m + kSlack)) {
-                const float up = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)));
-                const float f = m == -INFINITY ? 0.0f : exp2f(m - up);
-                m = up;
-                l *= f;
-#pragma unroll
-                for (int n = 0; n < DN; ++n) o[n] *= f;
-            }
-            const float base = (m == -INFINITY ? 0.0f : m) - drift;
-            now[0] = ahead[0], now[1] = ahead[1];
-
-            float sum[4] = {};
-            half8 p[4];
-            auto weigh = [&](int t) {
-                float w[8];
-#pragma unroll
-                for (int r = 0; r < 8; ++r) {
-                    w[r] = __builtin_amdgcn_exp2f(fmaf(now[t >> 1][8 * (t & 1) + r], c, -base));
-                    sum[r & 3] += w[r];
-                }
-                p[t] = half8{(_Float16)w[0], (_Float16)w[1], (_Float16)w[2], (_Float16)w[3], (_Float16)w[4], (_Float16)w[5], (_Float16)w[6], (_Float16)w[7]};
-            };
-            auto gather = [&](int n, int t) {
-                const half8 f = *(const half8 *)&tiles[side][buffer].values[padded<8>(32 * n + q32, 4 * (t >> 1) + 2 * h2 + (t & 1))];
-                o[n] = Mma<_Float16>::mma(f, p[t], o[n]);
-            };
-#pragma unroll
-            for (int kk = 0; kk < KK; ++kk) {
-                if constexpr (!last.value) {
-                    score(buffer ^ 1, 0, kk);
-                    score(buffer ^ 1, 1, kk);
-                }
-                if (kk % (KK / 4) == 0) weigh(kk / (KK / 4));
-            }
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int n = 0; n < DN; ++n) gather(n, t);
-            l = fmaf((sum[0] + sum[1]) + (sum[2] + sum[3]), undrift, l);
-            if constexpr (!last.value) {
-                hide(s1);
-                top = largest();
-                stage_keys(kc, buffer);
-                stage_values(s1, buffer ^ 1);
-                s0 = s1, s1 = s2;
-            }
+                for (int r = 0; r < 16; r += 2) x = most(x, most(ahead[kb][r], ahead[kb][r + 1]));
+            return x;
         };
-        int turn = from;
-        for (; turn + GROUPS < to; turn += GROUPS) take(turn, std::false_type{});
-        take(turn, std::true_type{});
-    }
+        auto score = [&](int buffer, int kb, int kk) {
+            const Frag f = *(const Frag *)&tiles[side][buffer].keys[padded<D / 8>(32 * kb + q32, 2 * kk + h2)];
+            ahead[kb] = Mma<T>::mma(f, q[kk], kk == 0 ? float16v{} : ahead[kb]);
+        };
 
-    // o[n][r]: query q32, channel 32 n + 8 (r / 4) + 4 h2 + r % 4, in units of 2^eref
-    const float unit = pow2(eref);
-    float4v x[DN][4];
-    l += __shfl_xor(l, 32);
+        if (from < to) {
+            const int page0 = page_of(from + side), page1 = page_of(from + side + GROUPS);
+            int page2 = page_of(from + side + 2 * GROUPS);
+            Step s0 = step_at(from + side, page0), s1 = step_at(from + side + GROUPS, page1);
+            {
+                Codes first;
+                fetch_keys(s0, first);
+                fetch_values(s0);
+                fetch_keys(s1, kc);
+                stage_keys(first, 0);
+                stage_values(s0, 0);
+                stage_keys(kc, 1);
+            }
+            __syncthreads();
 #pragma unroll
-    for (int n = 0; n < DN; ++n)
+            for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) x[n][r] = float4v{o[n][4 * r], o[n][4 * r + 1], o[n][4 * r + 2], o[n][4 * r + 3]} * unit;
-    if constexpr (GROUPS == 2) {
-        constexpr int kSums = DN * 4 * NT;
-        static_assert(sizeof(tiles) >= kSums * sizeof(float4v) + NT * sizeof(float2), "the sums go where keys and values were");
-        float4v *const sums = (float4v *)&tiles[0][0];
-        float2 *const ml = (float2 *)(sums + kSums);
-        __syncthreads();
-        if (side) {
-            ml[tid] = make_float2(m, l);
+                for (int kk = 0; kk < KK; ++kk) score(0, kb, kk);
+            hide(s0);
+            top = largest();
+            eref = __builtin_amdgcn_readfirstlane(exponent_of(s0.vs));
+
+            // one step; the last one looks at none behind it
+            auto take = [&](int turn, auto last) {
+                const int buffer = (turn - from) / GROUPS & 1, step = turn + side;
+                __syncthreads();  // keys of the next step and values of this one are there, and nobody reads what is written below
+                Step s2 = s1;
+                if constexpr (!last.value) {
+                    s2 = step_at(step + 2 * GROUPS, page2);
+                    page2 = page_of(step + 3 * GROUPS);
+                    fetch_keys(s2, kc);
+                    fetch_values(s1);
+                }
+
+                const float c = fmaxf(a.alpha * kLog2e * s0.ks, 1.17549435e-38f);
+                const int ev = __builtin_amdgcn_readfirstlane(exponent_of(s0.vs));
+                if (ev - eref > kDrift || eref - ev > kDrift) {
+                    const float f = pow2(eref - ev);
+                    eref = ev;
 #pragma unroll
-            for (int n = 0; n < DN; ++n)
+                    for (int n = 0; n < DN; ++n) o[n] *= f;
+                }
+                const float drift = (float)(ev - eref), undrift = pow2(eref - ev);
+                top *= c;
+                if (__any(top > m + kSlack)) {
+                    const float up = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)));
+                    const float f = m == -INFINITY ? 0.0f : exp2f(m - up);
+                    m = up;
+                    l *= f;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) sums[(n * 4 + r) * NT + tid] = x[n][r];
+                    for (int n = 0; n < DN; ++n) o[n] *= f;
+                }
+                const float base = (m == -INFINITY ? 0.0f : m) - drift;
+                now[0] = ahead[0], now[1] = ahead[1];
+
+                float sum[4] = {};
+                half8 p[4];
+                auto weigh = [&](int t) {
+                    float w[8];
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) {
+                        w[r] = __builtin_amdgcn_exp2f(fmaf(now[t >> 1][8 * (t & 1) + r], c, -base));
+                        sum[r & 3] += w[r];
+                    }
+                    p[t] = half8{(_Float16)w[0], (_Float16)w[1], (_Float16)w[2], (_Float16)w[3], (_Float16)w[4], (_Float16)w[5], (_Float16)w[6], (_Float16)w[7]};
+                };
+                auto gather = [&](int n, int t) {
+                    const half8 f = *(const half8 *)&tiles[side][buffer].values[padded<8>(32 * n + q32, 4 * (t >> 1) + 2 * h2 + (t & 1))];
+                    o[n] = Mma<_Float16>::mma(f, p[t], o[n]);
+                };
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk) {
+                    if constexpr (!last.value) {
+                        score(buffer ^ 1, 0, kk);
+                        score(buffer ^ 1, 1, kk);
+                    }
+                    if (kk % (KK / 4) == 0) weigh(kk / (KK / 4));
+                }
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int n = 0; n < DN; ++n) gather(n, t);
+                l = fmaf((sum[0] + sum[1]) + (sum[2] + sum[3]), undrift, l);
+                if constexpr (!last.value) {
+                    hide(s1);
+                    top = largest();
+                    stage_keys(kc, buffer);
+                    stage_values(s1, buffer ^ 1);
+                    s0 = s1, s1 = s2;
+                }
+            };
+            int turn = from;
+            for (; turn + GROUPS < to; turn += GROUPS) take(turn, std::false_type{});
+            take(turn, std::true_type{});
         }
-        __syncthreads();
-        if (side) return;
-        const float2 other = ml[tid];
-        top = fmaxf(m, other.x);
-        const float f = m == -INFINITY && l == 0.0f ? 0.0f : exp2f(m - top);  // a NaN among the scores stays one
-        const float g = other.x == -INFINITY && other.y == 0.0f ? 0.0f : exp2f(other.x - top);
-        m = top;
-        l = l * f + other.y * g;
+
+        // o[n][r]: query q32, channel 32 n + 8 (r / 4) + 4 h2 + r % 4, in units of 2^eref
+        const float unit = pow2(eref);
+        float4v x[DN][4];
+        l += __shfl_xor(l, 32);
 #pragma unroll
         for (int n = 0; n < DN; ++n)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) x[n][r] = x[n][r] * f + sums[(n * 4 + r) * NT + tid] * g;
+            for (int r = 0; r < 4; ++r) x[n][r] = float4v{o[n][4 * r], o[n][4 * r + 1], o[n][4 * r + 2], o[n][4 * r + 3]} * unit;
+        if constexpr (GROUPS == 2) {
+            constexpr int kSums = DN * 4 * NT;
+            static_assert(sizeof(tiles) >= kSums * sizeof(float4v) + NT * sizeof(float2), "the sums go where keys and values were");
+            float4v *const sums = (float4v *)&tiles[0][0];
+            float2 *const ml = (float2 *)(sums + kSums);
+            __syncthreads();
+            if (side) {
+                ml[tid] = make_float2(m, l);
+#pragma unroll
+                for (int n = 0; n < DN; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) sums[(n * 4 + r) * NT + tid] = x[n][r];
+            }
+            __syncthreads();
+            if (!side) {
+                const float2 other = ml[tid];
+                top = fmaxf(m, other.x);
+                const float f = m == -INFINITY && l == 0.0f ? 0.0f : exp2f(m - top);  // a NaN among the scores stays one
+                const float g = other.x == -INFINITY && other.y == 0.0f ? 0.0f : exp2f(other.x - top);
+                m = top;
+                l = l * f + other.y * g;
+#pragma unroll
+                for (int n = 0; n < DN; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[n][r] = x[n][r] * f + sums[(n * 4 + r) * NT + tid] * g;
+            }
+        }
+        if (has && !side) {
+            int64_t part = part0 + wave * R + q32;
+            if (part0 < 0) part = a.splits > 1 ? (blockIdx.x % a.splits) * (int64_t)a.seq.M * a.heads + (s.row + token) * a.heads + head * group + row - token * group : -1;
+#pragma unroll
+            for (int n = 0; n < DN; ++n)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) give<T, D>(a, s, head, group, part, row, 32 * n + 8 * r + 4 * h2, x[n][r], m, l, n == 0 && r == 0 && h2 == 0);
+        }
+
+        if (!SHARES || (left -= take) <= 0) return;
+        off = 0;
+        if (++tile_of_rows * kRows >= total) {
+            tile_of_rows = 0;
+            if (++head == H) {
+                head = 0;
+                do {
+                    if (++b >= a.seq.batch) return;  // only if the lengths change meanwhile
+                    s = sequence(a.seq, b);
+                } while (min(s.n, a.seq.max_new) <= 0);
+            }
+        }
+        __syncthreads();  // before the next tile's keys and values
     }
-    if (!has) return;
-    const int64_t part = a.splits > 1 ? split * (int64_t)a.seq.M * a.heads + (s.row + token) * a.heads + head * group + row - token * group : -1;
-#pragma unroll
-    for (int n = 0; n < DN; ++n)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) give<T, D>(a, s, head, group, part, row, 32 * n + 8 * r + 4 * h2, x[n][r], m, l, n == 0 && r == 0 && h2 == 0);
+}
+
+// The parts of rows that workgroups shared: who begins first inside a tile of rows joins what belongs to it.  D / 4 threads have
+// a row, four channels each.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void k_cache_attention_join_shares(CacheAttentionArgs a)
+{
+    constexpr int C = D / 4, kSide = 256 / C, kSplit = kTileRows / kSide;
+    const int share = blockIdx.x / kSplit + 1, at = blockIdx.x % kSplit * kSide + threadIdx.x / C, c = threadIdx.x % C;
+    const int4 *const begins = begins_of(a);
+    const int4 mine = begins[share], before = begins[share - 1];
+    auto inside = [&](int4 x) { return x.x == mine.x && x.y == mine.y && x.z == mine.z && x.w != 0; };
+    if (mine.x < 0 || mine.w == 0 || inside(before)) return;
+    const Seq s = sequence(a.seq, mine.x);
+    const int group = a.heads / a.cache.heads, row = mine.z * kTileRows + at;
+    if (row >= min(s.n, a.seq.max_new) * group) return;
+    const float2 *const ml = (const float2 *)(a.partial + a.part_rows * D);
+    float4v x = {};
+    float top = -INFINITY, sum = 0.0f;
+    for (int k = share - 1;;) {
+        const int64_t part = (2 * (int64_t)k + (k < share)) * kTileRows + at;
+        const float2 p = ml[part];
+        const float4v y = *(const float4v *)(a.partial + part * D + 4 * c);
+        const float up = fmaxf(top, p.x);
+        const float f = top == -INFINITY && sum == 0.0f ? 0.0f : exp2f(top - up);  // a NaN among the scores stays one
+        const float g = p.x == -INFINITY && p.y == 0.0f ? 0.0f : exp2f(p.x - up);
+        top = up;
+        sum = sum * f + p.y * g;
+        x = x * f + y * g;
+        if (++k >> a.share_log2 || !inside(begins[k])) break;
+    }
+    give<T, D>(a, s, mine.y, group, -1, row, 4 * c, x, top, sum, c == 0);
 }
 
 // The parts of a row: D / 4 threads have four channels each, ALONE of them a row for themselves (few parts, many rows), or
@@ -808,10 +953,17 @@ void launch(const CacheAttentionArgs &a, const AttentionPlan &plan, hipStream_t 
         // 40 / 56; chunks of up to 1024 tokens over 5163 to 16024 keys, four times, 641 / 610.
         constexpr int kMost = D <= 128 ? 2 : 1;
         const bool differ = a.seq.batch > 1 && a.seq.max_len >= 8192;
+        if constexpr (D <= 128) {
+            if (a.share_log2 >= 0) {
+                hipLaunchKernelGGL((k_cache_attention_rows<T, D, 1, true>), grid, block, 0, st, a, plan.row_tiles);
+                hipLaunchKernelGGL((k_cache_attention_join_shares<T, D>), dim3((((unsigned)1 << a.share_log2) - 1) * (kTileRows * D / 1024)), block, 0, st, a);
+                return;
+            }
+        }
         if (kMost == 2 && a.seq.max_len >= 1024 && plan.groups <= (differ ? 1024 : 512))
-            hipLaunchKernelGGL((k_cache_attention_rows<T, D, kMost>), grid, dim3(kMost * 256), 0, st, a, plan.row_tiles);
+            hipLaunchKernelGGL((k_cache_attention_rows<T, D, kMost, false>), grid, dim3(kMost * 256), 0, st, a, plan.row_tiles);
         else
-            hipLaunchKernelGGL((k_cache_attention_rows<T, D, 1>), grid, block, 0, st, a, plan.row_tiles);
+            hipLaunchKernelGGL((k_cache_attention_rows<T, D, 1, false>), grid, block, 0, st, a, plan.row_tiles);
     } else if (plan.rows == 16) {
         if (plan.waves == kAttWaves) hipLaunchKernelGGL((k_cache_attention<T, D, 1, kAttWaves>), grid, block, 0, st, a);
         else hipLaunchKernelGGL((k_cache_attention<T, D, 1, kTwice>), grid, dim3(kTwice * 64), 0, st, a);
@@ -875,6 +1027,20 @@ AttentionPlan cache_attention_plan(int M, int heads, int kv_heads, int dim, int 
         p.groups = 1 << p.share_log2;
         p.part_rows = (int64_t)2 * p.rows << p.share_log2;
         p.workspace = (size_t)p.part_rows * (dim + 2) * sizeof(float) + ((size_t)batch + 1) * sizeof(int);
+        return p;
+    }
+    // Few rounds of workgroups, each with many steps: the last round is often half empty, and sequences differ.  Two workgroups
+    // for every compute unit share all steps instead, unless rounds come out even or rows are so many that their ends differ
+    // (a prompt's: tiles are taken longest first then, and those that run at a time read the same keys, which shares do not).
+    // us, tiles / shares, 32 heads on 8 of 128: 1200 rows and 4096 keys 119 / 102; 512 and 8192, three times, 267 / 241; up to 1024
+    // and 5163 to 16024, four times, 595 / 538.  Against that 512 and 32768 keys four times 1131 / 1154, 512 and 2048 four times
+    // 78 / 95, a prompt of 8192 572 / 615, 2048 and 32768 four times 4292 / 4950; heads of 256 lose registers.
+    const double all = p.groups * (double)steps, rounds = p.groups / 256, fill = rounds / (double)(int64_t)(rounds + 255.0 / 256);
+    if (dim < 256 && steps >= 64 && p.groups > 256 && p.groups <= kMostShared && (int64_t)max_new * 2 <= max_len && (batch > 1 || fill < 0.85) && all < (double)(1u << 31)) {
+        p.share_log2 = 9;
+        p.groups = 1 << p.share_log2;
+        p.part_rows = (int64_t)2 * kTileRows << p.share_log2;
+        p.workspace = (size_t)p.part_rows * (dim + 2) * sizeof(float) + (sizeof(int4) << p.share_log2);
         return p;
     }
     // Parts of many rows are large: only for a workgroup on every compute unit, and of 16 steps at least.

@@ -509,3 +509,30 @@ def test_two_graphs_in_turn():
 def test_sequences_of_eight_to_eleven_steps(dim, heads, kv, dtype, window):
     """So long that a workgroup of twice the wavefronts has one, a last step that holds one key, one sequence without any."""
     case(41 + dim + heads, [513, 700, 0, 20], [1, 1, 0, 1], heads, kv, 64, dim, dtype, True, window)
+
+
+@pytest.mark.parametrize("dim,group,dtype,causal,window", [(128, 2, f16, True, 0), (64, 3, b16, True, 0), (128, 1, b16, False, 0), (64, 2, f16, True, 90), (128, 5, f16, True, 300)])
+def test_equal_shares_of_many_rows(dim, group, dtype, causal, window):
+    """Tiles of rows whose steps workgroups share: shares begin and end inside a tile, hold several tiles, heads and sequences, a
+    long tile belongs to many, and sequences of no rows or no tokens lie between."""
+    g = torch.Generator().manual_seed(dim + group)
+    batch, kv, max_new = 52, 3, 70 if group < 5 else 30
+    lens = [int(torch.randint(0, 40, (1,), generator=g)) * int(torch.randint(0, 5, (1,), generator=g)) for _ in range(batch)]
+    lens[0], lens[20], lens[21], lens[51] = 0, 1700, 0, 900
+    new = [int(torch.randint(0, 12, (1,), generator=g)) for _ in range(batch)]
+    new[0], new[20], new[21], new[33], new[51] = 3, max_new, 0, 0, max_new
+    case(51 + group, lens, new, kv * group, kv, 64, dim, dtype, causal, window, max_new=max(max_new, -(-129 // group)), max_len=5000)
+
+
+def test_equal_shares_of_one_sequence():
+    """Fewer tiles than the host's bound allows, so that a tile is many workgroups', and fewer steps than workgroups."""
+    for lens, new in (([1100], [100]), ([60], [3]), ([64], [64])):
+        case(61, lens, new, 40, 40, 128, 64, f16, max_new=1000, max_len=6000)
+
+
+def test_equal_shares_without_rows():
+    g = torch.Generator().manual_seed(62)
+    ref, table = filled(g, [90] * 50, 3, 64, 128)
+    Q = torch.randn((4, 6, 128), generator=g).half()
+    got = run(ref, ref.device(B), Q, table, [90] * 50, [0] * 50, 6, 0.1, True, 0, max_new=100, max_len=5000)
+    assert (got[0] == 33).all() and (got[1] == 33).all()
