@@ -238,3 +238,12 @@ def test_the_same_bits_twice():
     torch.cuda.synchronize()
     for a, b in zip(caches[0].tensors, caches[1].tensors):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("block", [64, 128, 256])
+def test_every_block_and_head_size_of_both_types(block, dim, dtype):
+    """A prompt that ends inside a block, tokens one by one over the block's end, a chunk."""
+    test_writes_in_a_row_and_reads(block, dim, 2, dtype, [(0, [block + 3, 1, 7]), (0, [block - 1, 1, block])])
+    test_writes_in_a_row_and_reads(block, dim, 1, dtype, [(0, [1, 1]), (0, [1, 1])])

@@ -536,3 +536,11 @@ def test_equal_shares_without_rows():
     Q = torch.randn((4, 6, 128), generator=g).half()
     got = run(ref, ref.device(B), Q, table, [90] * 50, [0] * 50, 6, 0.1, True, 0, max_new=100, max_len=5000)
     assert (got[0] == 33).all() and (got[1] == 33).all()
+
+
+@pytest.mark.parametrize("dtype", [f16, b16])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("group", [1, 20])
+@pytest.mark.parametrize("max_len", [250, 640, 2560])  # a workgroup of four wavefronts for each head, of eight, parts that are joined
+def test_every_head_size_of_both_types(max_len, group, dim, dtype):
+    case(71 + dim + group, [250, 33], [1, 1], 2 * group, 2, 64, dim, dtype, max_len=max_len)

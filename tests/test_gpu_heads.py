@@ -105,3 +105,10 @@ def test_many_heads_are_spread_and_many_tokens_are_not():
     torch.cuda.synchronize()
     for m in range(0, M, 997):
         assert torch.equal(whole[0][m], single[0][m]) and torch.equal(whole[1][m], single[1][m])
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("dim", [16, 32, 48, 64, 128, 256])
+def test_every_head_size_of_both_types_and_orders(dim, inter, dtype):
+    test_against_64_bits(17, 3, 2, dim, dim // 32 * 16 or 16, inter, True, dtype)
