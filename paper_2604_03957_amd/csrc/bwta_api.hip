@@ -647,7 +647,7 @@ int bwta_cache_read(const bwta_cache *cache, void *K, int64_t ldk, void *V, int6
 size_t bwta_cache_attention_workspace_bytes(int M, int heads, int kv_heads, int dim, int batch, int max_new, int max_len)
 {
     if (M <= 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || heads > kMostHeads || dim <= 0 || dim > 256 || batch <= 0 || max_new <= 0 || max_len <= 0) return 0;
-    return round_up(bwta::cache_attention_plan(M, heads, kv_heads, dim, batch, max_new, max_len).workspace, 256);
+    return round_up(bwta::cache_attention_plan(heads, kv_heads, dim, batch, max_new, max_len).workspace, 256);
 }
 
 int bwta_cache_attention(const bwta_cache *cache, const void *Q, int64_t ldq, void *out, int64_t ldo, int dtype, float *lse,
@@ -670,7 +670,7 @@ int bwta_cache_attention(const bwta_cache *cache, const void *Q, int64_t ldq, vo
     if (need && (!workspace || workspace_bytes < need)) return BWTA_ERR_WORKSPACE;
     if (need && !aligned(workspace, 256)) return BWTA_ERR_ALIGN;
     const bwta::SeqArgs s{table, ldt, lens, cu, batch, M, max_new, max_len};
-    const bwta::AttentionPlan plan = bwta::cache_attention_plan(M, heads, cache->kv_heads, cache->dim, batch, max_new, max_len);
+    const bwta::AttentionPlan plan = bwta::cache_attention_plan(heads, cache->kv_heads, cache->dim, batch, max_new, max_len);
     if (plan.groups > kMostGroups || (double)max_new * (heads / cache->kv_heads) > (1u << 31) - 1024.0 || (plan.workspace && (double)batch * max_new * heads > kMostGroups))
         return BWTA_ERR_TOO_LARGE;
     return hip_result(bwta::launch_cache_attention({cache_args(cache), s, Q, out, ldq, ldo, lse, heads, alpha, causal != 0, dtype == BWTA_DTYPE_BF16, window,

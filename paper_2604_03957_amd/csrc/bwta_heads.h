@@ -165,7 +165,7 @@ struct CacheAttentionArgs {
     bool causal, bf16;
     int window;
     // Parts of rows that are joined afterwards: [part_rows][dim] sums, then [part_rows][2] maximum and sum of weights.  Many
-    // rows: [splits][M * heads].  Few (share_rows of them a workgroup): [batch * key heads][splits][share_rows], or where
+    // rows: [splits][batch * max_new * heads].  Few (share_rows of them a workgroup): [batch * key heads][splits][share_rows], or where
     // 2^share_log2 workgroups share all steps (-1: they do not) [workgroups][2][share_rows], and behind the parts how many
     // steps lie before each sequence.
     float *partial;
@@ -178,7 +178,7 @@ struct AttentionPlan {
     int64_t part_rows;
     size_t workspace;  // bytes
 };
-AttentionPlan cache_attention_plan(int M, int heads, int kv_heads, int dim, int batch, int max_new, int max_len);
+AttentionPlan cache_attention_plan(int heads, int kv_heads, int dim, int batch, int max_new, int max_len);
 hipError_t launch_cache_attention(CacheAttentionArgs a, const AttentionPlan &plan, hipStream_t st);
 
 }  // namespace bwta

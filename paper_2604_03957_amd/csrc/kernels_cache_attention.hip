@@ -119,7 +119,7 @@ __device__ __forceinline__ int *shares_of(const CacheAttentionArgs &a) { return 
 // needs in registers and nothing in LDS until their sums are joined; 16 rows is what the matrix cores take anyway, so heads that
 // share their keys cost nothing.  Bound by the cache's bytes: 64 sequences of 2048 to 8192 tokens, 32 heads on 8 of 128 (680 MB)
 // take 118 us, 5.7 TB/s, equal ones of 8192 6.4 TB/s; one token over 131072 keys (268 MB) 49.5 us with the join, over 2048 keys
-// of 32 heads (17 MB) 11.2 us, most of it the latency of lengths, table and codes one after the other, and of a second launch.
+// of 32 heads (17 MB) 9.8 us, most of it the latency of lengths, table and codes one after the other, and of a second launch.
 template <typename T, int D, int NB, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_cache_attention(CacheAttentionArgs a)
 {
@@ -786,7 +786,7 @@ __global__ __launch_bounds__(GROUPS * 256, D <= 128 ? 2 : 1) void k_cache_attent
         }
         if (has && !side) {
             int64_t part = part0 + wave * R + q32;
-            if (part0 < 0) part = a.splits > 1 ? (blockIdx.x % a.splits) * (int64_t)a.seq.M * a.heads + (s.row + token) * a.heads + head * group + row - token * group : -1;
+            if (part0 < 0) part = a.splits > 1 ? ((int64_t)(blockIdx.x % a.splits) * a.seq.batch + b) * a.seq.max_new * a.heads + (int64_t)token * a.heads + head * group + row - token * group : -1;
 #pragma unroll
             for (int n = 0; n < DN; ++n)
 #pragma unroll
@@ -844,6 +844,8 @@ __global__ __launch_bounds__(256) void k_cache_attention_join_shares(CacheAttent
 // The parts of a row: D / 4 threads have four channels each, ALONE of them a row for themselves (few parts, many rows), or
 // all of a workgroup's threads one row, each D / 4 some of its parts.
 constexpr int kFewSplits = 8, kMostParts = 1024;
+// A small kernel: what it takes is the latency of its loads, so all that can leave at once do (one token over 2048 keys in eight
+// parts 11.2 -> 9.8 us with both launches).
 template <typename T, int D, bool ALONE>
 __global__ __launch_bounds__(256) void k_cache_attention_join(CacheAttentionArgs a)
 {
@@ -861,15 +863,15 @@ __global__ __launch_bounds__(256) void k_cache_attention_join(CacheAttentionArgs
         units_before = shares[b], units = shares[b + 1] - units_before, units_all = shares[a.seq.batch];
     }
     const Seq s = sequence(a.seq, b);
-    if (t >= s.n) return;
-    const int64_t row = (int64_t)(s.row + t) * a.heads + h;
-    // the row's parts: the first, and from the second on every `stride`-th
+    // The row's parts: the first, and from the second on every `stride`-th.  (Unless work was shared the lengths say nothing about
+    // them, so they are asked for together with those.)
     const int H = a.cache.heads, group = a.heads / H, r = t * group + h % group;
-    int64_t first = row, stride = (int64_t)a.seq.M * a.heads;
+    int64_t first = item, stride = (int64_t)a.seq.batch * a.seq.max_new * a.heads;
     if (a.share_rows <= 32) first = ((int64_t)(b * H + h / group) * a.splits) * a.share_rows + r, stride = a.share_rows;
     int64_t second = first + stride;
     int parts = a.splits;
     if (shared) {
+        if (t >= s.n) return;
         const int u = units_before * H + h / group * units, total = units_all * H, log2 = shares_log2(a, total);
         auto owner = [&](int x) {  // the workgroup whose share holds step x; the quotient is at most one off
             int w = (int)(((double)x + 0.5) * (double)(1 << log2) / (double)total);
@@ -891,25 +893,36 @@ __global__ __launch_bounds__(256) void k_cache_attention_join(CacheAttentionArgs
     auto factor = [&](float2 p) { return p.x == -INFINITY && p.y == 0.0f ? 0.0f : exp2f(p.x - top); };  // a NaN among the scores stays one
     if constexpr (ALONE) {
         float2 p[kFewSplits];
+        float4v y[kFewSplits];
 #pragma unroll
         for (int k = 0; k < kFewSplits; ++k) {
-            p[k] = k < parts ? ml[at(k)] : make_float2(-INFINITY, 0.0f);
+            const int64_t part = at(min(k, parts - 1));
+            p[k] = ml[part];
+            y[k] = *(const float4v *)(o + part * D);
+        }
+        if (t >= s.n) return;
+#pragma unroll
+        for (int k = 0; k < kFewSplits; ++k) {
+            if (k >= parts) p[k] = make_float2(-INFINITY, 0.0f), y[k] = float4v{};
             top = fmaxf(top, p[k].x);
         }
 #pragma unroll
         for (int k = 0; k < kFewSplits; ++k) {
-            if (k >= parts) break;
             const float f = factor(p[k]);
             sum = fmaf(f, p[k].y, sum);
-            x += *(const float4v *)(o + at(k) * D) * f;
+            x += y[k] * f;
         }
     } else {
+        constexpr int kEarly = 8;  // of a thread's parts, asked for before anything is known about them
         float2 p[kMostParts / 256];
+        float4v early[kEarly];
 #pragma unroll
-        for (int j = 0; j < kMostParts / 256; ++j) {
-            p[j] = tid + 256 * j < parts ? ml[at(tid + 256 * j)] : make_float2(-INFINITY, 0.0f);
-            top = fmaxf(top, p[j].x);
-        }
+        for (int j = 0; j < kMostParts / 256; ++j) p[j] = tid + 256 * j < parts ? ml[at(tid + 256 * j)] : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+        for (int j = 0; j < kEarly; ++j) early[j] = nth + j * kSide < parts ? *(const float4v *)(o + at(nth + j * kSide) * D) : float4v{};
+        if (t >= s.n) return;
+#pragma unroll
+        for (int j = 0; j < kMostParts / 256; ++j) top = fmaxf(top, p[j].x);
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
         if ((tid & 63) == 0) some[0][tid >> 6] = top;
@@ -926,8 +939,11 @@ __global__ __launch_bounds__(256) void k_cache_attention_join(CacheAttentionArgs
         if ((tid & 63) == 0) some[1][tid >> 6] = sum;
         __syncthreads();
         sum = (some[1][0] + some[1][1]) + (some[1][2] + some[1][3]);
+#pragma unroll
+        for (int j = 0; j < kEarly; ++j)
+            if (nth + j * kSide < parts) x += early[j] * weight[nth + j * kSide];
 #pragma unroll 4
-        for (int k = nth; k < parts; k += kSide) x += *(const float4v *)(o + at(k) * D) * weight[k];
+        for (int k = nth + kEarly * kSide; k < parts; k += kSide) x += *(const float4v *)(o + at(k) * D) * weight[k];
         side[nth][c] = x;
         __syncthreads();
         if (nth) return;
@@ -935,8 +951,9 @@ __global__ __launch_bounds__(256) void k_cache_attention_join(CacheAttentionArgs
         for (int k = 1; k < kSide; ++k) x += side[k][c];
     }
     const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
-    *(uint2 *)((T *)a.out + (s.row + t) * a.ldo + (int64_t)h * D + 4 * c) = make_uint2(Half<T>::pack(x[0] * f, x[1] * f), Half<T>::pack(x[2] * f, x[3] * f));
-    if (c == 0 && a.lse) a.lse[row] = kLn2 * (top + log2f(sum));
+    const int64_t token = s.row + t;
+    *(uint2 *)((T *)a.out + token * a.ldo + (int64_t)h * D + 4 * c) = make_uint2(Half<T>::pack(x[0] * f, x[1] * f), Half<T>::pack(x[2] * f, x[3] * f));
+    if (c == 0 && a.lse) a.lse[token * a.heads + h] = kLn2 * (top + log2f(sum));
 }
 
 constexpr int kAttWaves = 4;
@@ -990,7 +1007,7 @@ void launch_type(const CacheAttentionArgs &a, const AttentionPlan &plan, hipStre
 
 }  // namespace
 
-AttentionPlan cache_attention_plan(int M, int heads, int kv_heads, int dim, int batch, int max_new, int max_len)
+AttentionPlan cache_attention_plan(int heads, int kv_heads, int dim, int batch, int max_new, int max_len)
 {
     AttentionPlan p{};
     const int64_t rows = (int64_t)max_new * (heads / kv_heads), steps = ((int64_t)max_len + kCacheTile - 1) / kCacheTile;
@@ -1048,7 +1065,7 @@ AttentionPlan cache_attention_plan(int M, int heads, int kv_heads, int dim, int 
     if (s <= 1) return p;
     p.splits = (int)s;
     p.groups *= p.splits;
-    p.part_rows = (int64_t)p.splits * M * heads;
+    p.part_rows = (int64_t)p.splits * batch * max_new * heads;
     p.workspace = (size_t)p.part_rows * (dim + 2) * sizeof(float);
     return p;
 }
