@@ -670,7 +670,12 @@ int bwta_cache_attention(const bwta_cache *cache, const void *Q, int64_t ldq, vo
     if (need && (!workspace || workspace_bytes < need)) return BWTA_ERR_WORKSPACE;
     if (need && !aligned(workspace, 256)) return BWTA_ERR_ALIGN;
     const bwta::SeqArgs s{table, ldt, lens, cu, batch, M, max_new, max_len};
-    const bwta::AttentionPlan plan = bwta::cache_attention_plan(heads, cache->kv_heads, cache->dim, batch, max_new, max_len);
+    bwta::AttentionPlan plan = bwta::cache_attention_plan(heads, cache->kv_heads, cache->dim, batch, max_new, max_len);
+    const int64_t reach = (int64_t)window + max_new + 62;  // the workspace is for any window, so a plan for this one has to fit it
+    if (window && reach < max_len) {
+        const bwta::AttentionPlan near = bwta::cache_attention_plan(heads, cache->kv_heads, cache->dim, batch, max_new, (int)reach);
+        if (near.workspace <= plan.workspace) plan = near;
+    }
     if (plan.groups > kMostGroups || (double)max_new * (heads / cache->kv_heads) > (1u << 31) - 1024.0 || (plan.workspace && (double)batch * max_new * heads > kMostGroups))
         return BWTA_ERR_TOO_LARGE;
     return hip_result(bwta::launch_cache_attention({cache_args(cache), s, Q, out, ldq, ldo, lse, heads, alpha, causal != 0, dtype == BWTA_DTYPE_BF16, window,

@@ -33,20 +33,24 @@ struct Seq {
 __device__ __forceinline__ Seq sequence(const SeqArgs &a, int b)
 {
     Seq s;
-    const int len = a.lens[b];
-    int lo, hi;
-    if (a.cu) {
-        lo = min(max(a.cu[b], 0), a.M);
-        hi = min(max(a.cu[b + 1], lo), a.M);
-    } else {
-        lo = b * a.max_new;  // the host has checked batch * max_new <= M
-        hi = lo + a.max_new;
-    }
+    // (all loads at once, without a branch before any)
+    const int32_t *const offsets = a.cu ? a.cu : a.lens;
+    const int len = a.lens[b], begin = offsets[b], end = offsets[a.cu ? b + 1 : b];
+    const int lo = a.cu ? min(max(begin, 0), a.M) : b * a.max_new;  // the host has checked batch * max_new <= M
+    const int hi = a.cu ? min(max(end, lo), a.M) : lo + a.max_new;
     s.row = lo;
     s.n = hi - lo;
     s.len = min(max(len, 0), a.max_len);
     s.start = s.len - s.n;
     return s;
+}
+
+// The same for a whole wavefront's sequence, in scalar registers (the kernels of many rows have no others left: in vector registers
+// chunks of long prompts took 687 us, so 532).
+__device__ __forceinline__ Seq sequence_of_all(const SeqArgs &a, int b)
+{
+    const Seq s = sequence(a, b);
+    return {__builtin_amdgcn_readfirstlane(s.row), __builtin_amdgcn_readfirstlane(s.n), __builtin_amdgcn_readfirstlane(s.len), __builtin_amdgcn_readfirstlane(s.start)};
 }
 
 template <typename T> struct Half;  // what differs between the two 16-bit types
@@ -174,11 +178,12 @@ struct CacheAttentionArgs {
 };
 struct AttentionPlan {
     int rows, row_tiles, splits, share_log2, waves;
+    int reach;  // keys that the rows of a sequence see at most
     double groups;  // workgroups
     int64_t part_rows;
     size_t workspace;  // bytes
 };
-AttentionPlan cache_attention_plan(int heads, int kv_heads, int dim, int batch, int max_new, int max_len);
+AttentionPlan cache_attention_plan(int heads, int kv_heads, int dim, int batch, int max_new, int reach);
 hipError_t launch_cache_attention(CacheAttentionArgs a, const AttentionPlan &plan, hipStream_t st);
 
 }  // namespace bwta

@@ -118,8 +118,8 @@ __device__ __forceinline__ int *shares_of(const CacheAttentionArgs &a) { return 
 // Few rows (decoding): a workgroup has all NB * 16, and its wavefronts take turns at the steps of 64 keys, each with what it
 // needs in registers and nothing in LDS until their sums are joined; 16 rows is what the matrix cores take anyway, so heads that
 // share their keys cost nothing.  Bound by the cache's bytes: 64 sequences of 2048 to 8192 tokens, 32 heads on 8 of 128 (680 MB)
-// take 118 us, 5.7 TB/s, equal ones of 8192 6.4 TB/s; one token over 131072 keys (268 MB) 49.5 us with the join, over 2048 keys
-// of 32 heads (17 MB) 9.8 us, most of it the latency of lengths, table and codes one after the other, and of a second launch.
+// take 119 us, 5.7 TB/s, equal ones of 8192 6.4 TB/s; one token over 131072 keys (268 MB) 48.8 us with the join, over 2048 keys
+// of 32 heads (17 MB) 9.7 us, most of it the latency of lengths, table and codes one after the other, and of a second launch.
 template <typename T, int D, int NB, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_cache_attention(CacheAttentionArgs a)
 {
@@ -459,7 +459,7 @@ __global__ __launch_bounds__(GROUPS * 256, D <= 128 ? 2 : 1) void k_cache_attent
         const int round = (int)(i / (a.seq.batch * H)), bh = i % (a.seq.batch * H);
         head = bh % H, b = (bh / H + round) % a.seq.batch;
         tile_of_rows = row_tiles - 1 - round;
-        s = sequence(a.seq, b);
+        s = sequence_of_all(a.seq, b);
         if (tile_of_rows * kRows >= min(s.n, a.seq.max_new) * group) return;
     } else {
         // steps of each sequence, for one head
@@ -504,7 +504,7 @@ __global__ __launch_bounds__(GROUPS * 256, D <= 128 ? 2 : 1) void k_cache_attent
             }
             at += of;
         }
-        s = sequence(a.seq, b);
+        s = sequence_of_all(a.seq, b);
         const int total = min(s.n, a.seq.max_new) * group, last_tile = (total - 1) / kRows;
         for (tile_of_rows = 0;; tile_of_rows += 64) {
             const int tile = tile_of_rows + lane, units = tile <= last_tile ? rows_reach(a, s, group, total, tile).units : 0;
@@ -801,7 +801,7 @@ __global__ __launch_bounds__(GROUPS * 256, D <= 128 ? 2 : 1) void k_cache_attent
                 head = 0;
                 do {
                     if (++b >= a.seq.batch) return;  // only if the lengths change meanwhile
-                    s = sequence(a.seq, b);
+                    s = sequence_of_all(a.seq, b);
                 } while (min(s.n, a.seq.max_new) <= 0);
             }
         }
@@ -969,7 +969,7 @@ void launch(const CacheAttentionArgs &a, const AttentionPlan &plan, hipStream_t 
         // heads of 128: a causal prompt of 2048 with 32 heads 58 / 55, two of them 95 / 109; 128 rows over 256 keys, 32 times,
         // 40 / 56; chunks of up to 1024 tokens over 5163 to 16024 keys, four times, 641 / 610.
         constexpr int kMost = D <= 128 ? 2 : 1;
-        const bool differ = a.seq.batch > 1 && a.seq.max_len >= 8192;
+        const bool differ = a.seq.batch > 1 && plan.reach >= 8192;
         if constexpr (D <= 128) {
             if (a.share_log2 >= 0) {
                 hipLaunchKernelGGL((k_cache_attention_rows<T, D, 1, true>), grid, block, 0, st, a, plan.row_tiles);
@@ -977,7 +977,7 @@ void launch(const CacheAttentionArgs &a, const AttentionPlan &plan, hipStream_t 
                 return;
             }
         }
-        if (kMost == 2 && a.seq.max_len >= 1024 && plan.groups <= (differ ? 1024 : 512))
+        if (kMost == 2 && plan.reach >= 1024 && plan.groups <= (differ ? 1024 : 512))
             hipLaunchKernelGGL((k_cache_attention_rows<T, D, kMost, false>), grid, dim3(kMost * 256), 0, st, a, plan.row_tiles);
         else
             hipLaunchKernelGGL((k_cache_attention_rows<T, D, 1, false>), grid, block, 0, st, a, plan.row_tiles);
@@ -1007,16 +1007,16 @@ void launch_type(const CacheAttentionArgs &a, const AttentionPlan &plan, hipStre
 
 }  // namespace
 
-AttentionPlan cache_attention_plan(int heads, int kv_heads, int dim, int batch, int max_new, int max_len)
+AttentionPlan cache_attention_plan(int heads, int kv_heads, int dim, int batch, int max_new, int reach)
 {
     AttentionPlan p{};
-    const int64_t rows = (int64_t)max_new * (heads / kv_heads), steps = ((int64_t)max_len + kCacheTile - 1) / kCacheTile;
+    const int64_t rows = (int64_t)max_new * (heads / kv_heads), steps = ((int64_t)reach + kCacheTile - 1) / kCacheTile;
     const double parts = (double)batch * kv_heads;  // sequences times key heads
     // rows of a workgroup: up to 16 or 32 that its four wavefronts share, else 32 for each of four (or of twice four)
     p.rows = rows <= 16 ? 16 : rows <= 32 && dim < 256 ? 32 : 128;
     p.row_tiles = (int)((rows + p.rows - 1) / p.rows);
     p.groups = (double)p.row_tiles * parts;
-    p.splits = 1, p.share_log2 = -1, p.waves = kAttWaves;
+    p.splits = 1, p.share_log2 = -1, p.waves = kAttWaves, p.reach = reach;
     if (p.rows <= 32) {
         // Two workgroups for every compute unit, as long as each of their wavefronts still has a step: every sequence is split
         // into as many parts, and a long one's take longer, which is little where they are short (us, a token over 131072 keys
@@ -1050,18 +1050,20 @@ AttentionPlan cache_attention_plan(int heads, int kv_heads, int dim, int batch, 
     // for every compute unit share all steps instead, unless rounds come out even or rows are so many that their ends differ
     // (a prompt's: tiles are taken longest first then, and those that run at a time read the same keys, which shares do not).
     // us, tiles / shares, 32 heads on 8 of 128: 1200 rows and 4096 keys 119 / 102; 512 and 8192, three times, 267 / 241; up to 1024
-    // and 5163 to 16024, four times, 595 / 538.  Against that 512 and 32768 keys four times 1131 / 1154, 512 and 2048 four times
+    // and 5163 to 16024, four times, 595 / 532.  Against that 512 and 32768 keys four times 1131 / 1154, 512 and 2048 four times
     // 78 / 95, a prompt of 8192 572 / 615, 2048 and 32768 four times 4292 / 4950; heads of 256 lose registers.
     const double all = p.groups * (double)steps, rounds = p.groups / 256, fill = rounds / (double)(int64_t)(rounds + 255.0 / 256);
-    if (dim < 256 && steps >= 64 && p.groups > 256 && p.groups <= kMostShared && (int64_t)max_new * 2 <= max_len && (batch > 1 || fill < 0.85) && all < (double)(1u << 31)) {
+    if (dim < 256 && steps >= 64 && p.groups > 256 && p.groups <= kMostShared && (int64_t)max_new * 2 <= reach && (batch > 1 || fill < 0.85) && all < (double)(1u << 31)) {
         p.share_log2 = 9;
         p.groups = 1 << p.share_log2;
         p.part_rows = (int64_t)2 * kTileRows << p.share_log2;
         p.workspace = (size_t)p.part_rows * (dim + 2) * sizeof(float) + (sizeof(int4) << p.share_log2);
         return p;
     }
-    // Parts of many rows are large: only for a workgroup on every compute unit, and of 16 steps at least.
-    const int64_t want = p.groups >= 256 ? 1 : (int64_t)((256 + p.groups - 1) / p.groups), most = steps / 16, s = want < most ? want : most;
+    // Parts of many rows are large: one round of workgroups at most, and four steps each at least.  (us, 100 rows and 2000 keys of
+    // 8 heads 15.9, with 16 steps 27.1; 33 rows of 8 heads on 2, 32768 keys 23.1 and 29.4; 88 rows of 36 heads and sequences, 6200
+    // keys, six parts each 31, eight, which are more than a round, 47.)
+    const int64_t want = (int64_t)(256 / p.groups), most = steps / 4, s = want < most ? want : most;
     if (s <= 1) return p;
     p.splits = (int)s;
     p.groups *= p.splits;

@@ -544,3 +544,19 @@ def test_equal_shares_without_rows():
 @pytest.mark.parametrize("max_len", [250, 640, 2560])  # a workgroup of four wavefronts for each head, of eight, parts that are joined
 def test_every_head_size_of_both_types(max_len, group, dim, dtype):
     case(71 + dim + group, [250, 33], [1, 1], 2 * group, 2, 64, dim, dtype, max_len=max_len)
+
+
+@pytest.mark.parametrize("new", [[1, 1, 1], [5, 2, 1], [60, 3, 40]])
+@pytest.mark.parametrize("window", [1, 63, 64, 700, 1100])
+def test_windows_far_inside_long_sequences(new, window):
+    """The work is laid out for what a window lets rows see, in a workspace for any."""
+    for max_len in (2300, 20000):
+        case(81 + window, [2300, 64, 1200], new, 4, 2, 64, 128, f16, True, window, max_len=max_len)
+    case(82 + window, [2300, 64, 1200], new, 8, 8, 128, 64, b16, True, window, max_len=200000)
+
+
+@pytest.mark.parametrize("dim,heads,kv,lens,new,dtype", [(128, 8, 8, [1990], [100], f16), (256, 4, 4, [700, 300], [170, 200], b16), (64, 6, 2, [1500, 300, 40], [30, 22, 40], f16), (128, 24, 6, [900], [22], b16)])
+def test_many_rows_in_short_parts(dim, heads, kv, lens, new, dtype):
+    """Parts of four steps and more, up to one round of workgroups."""
+    case(91 + dim, lens, new, heads, kv, 64, dim, dtype)
+    case(92 + dim, lens, new, heads, kv, 64, dim, dtype, False)
