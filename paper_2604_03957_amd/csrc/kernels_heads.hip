@@ -25,7 +25,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_head_norm_rope(HeadRopeArgs a, 
     const int64_t m = item / chunks;
     const int chunk = (int)(item - m * chunks);
     const int half = a.rot / 2;
-    if (m < a.M) {
+    if (m < a.M && half > 0) {  // without a rotation there need be no positions
         const double pos = (double)a.positions[m];
         for (int p = lane; p < half; p += 64) {
             const double turns = pos * (double)a.inv_freq[p] * 0.15915494309189533577;

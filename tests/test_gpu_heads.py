@@ -112,3 +112,14 @@ def test_many_heads_are_spread_and_many_tokens_are_not():
 @pytest.mark.parametrize("dim", [16, 32, 48, 64, 128, 256])
 def test_every_head_size_of_both_types_and_orders(dim, inter, dtype):
     test_against_64_bits(17, 3, 2, dim, dim // 32 * 16 or 16, inter, True, dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_the_norm_alone_needs_no_positions(dtype):
+    g = torch.Generator().manual_seed(6)
+    x, w = torch.randn((9, 3, 80), generator=g).to(dtype), (1 + torch.rand(80, generator=g)).to(dtype)
+    out = torch.empty((9, 3, 80), dtype=dtype, device=DEV)
+    B.bwta_head_norm_rope(x.to(DEV), None, w.to(DEV), None, None, None, out, None, M=9, heads=3, kv_heads=0, dim=80, rot_dim=0)
+    torch.cuda.synchronize()
+    want, size = R.rope(x, w, None, None, 0, False, 1e-6, True)
+    _close(out, want, size, dtype)
