@@ -345,7 +345,7 @@ typedef struct bwta_cache {
  * max_new rows each (batch * max_new <= M).  They are its LAST tokens: lens[b] (int32 [batch]) counts
  * the sequence's tokens with them, so row cu[b] + i is token lens[b] - n_b + i, n_b = cu[b + 1] - cu[b].
  *   M        rows of the dense arrays; rows of no sequence are neither read nor written
- *   max_new  at least every n_b: rows behind it are left out;  max_len  at least every lens[b]:
+ *   max_new  at least every n_b: rows behind it are left out (above M it counts as M);  max_len  at least every lens[b]:
  *            larger ones count as max_len; at most 2^28 (BWTA_ERR_TOO_LARGE).  Both are the host's
  *            bounds for the launch; a captured graph may be replayed with other lens, cu and table
  *            contents inside them.

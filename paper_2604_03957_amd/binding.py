@@ -430,14 +430,31 @@ def bwta_gemm_grouped(problem_array, workspace, *, M, N, K, a_scale_mode=SCALE_V
 # ---- operators on heads ------------------------------------------------------------------------------
 
 
-def _dtype(x, dtype):
-    """The dtype argument of an operator on heads: as given, or the tensor's."""
+def _dtype(dtype, x, *others):
+    """The dtype argument of an operator on heads: as given, or the tensors', whose rows have no gaps between elements."""
+    for y in (x, *others):
+        if isinstance(y, torch.Tensor) and y.dim() and y.stride(-1) != 1 and y.shape[-1] > 1:
+            raise ValueError("elements of a row lie next to each other, got strides %s" % (tuple(y.stride()),))
     if dtype is not None:
         return dtype
     try:
-        return {torch.float16: DTYPE_FP16, torch.bfloat16: DTYPE_BF16}[x.dtype]
+        given = {torch.float16: DTYPE_FP16, torch.bfloat16: DTYPE_BF16}[x.dtype]
     except (AttributeError, KeyError):
         raise TypeError("pass dtype= with addresses; tensors are float16 or bfloat16, got %s" % getattr(x, "dtype", type(x).__name__)) from None
+    for y in others:
+        if isinstance(y, torch.Tensor) and y.dtype != x.dtype:
+            raise TypeError("tensors of one type, got %s beside %s" % (y.dtype, x.dtype))
+    return given
+
+
+def _dense(dtype, *xs):
+    """Positions, lengths, offsets, frequencies and the like are what the header says, one after the other."""
+    for x in xs:
+        if isinstance(x, torch.Tensor):
+            if x.dtype != dtype:
+                raise TypeError("a tensor of %s has to be %s" % (x.dtype, dtype))
+            if not x.is_contiguous():
+                raise ValueError("a tensor of strides %s has to be contiguous" % (tuple(x.stride()),))
 
 
 def _here(*xs):
@@ -477,15 +494,20 @@ def bwta_head_norm_rope(Q, K, wq, wk, positions, inv_freq, Qout, Kout, *, M, hea
                         norm=True, interleaved=False, ldq=None, ldk=None, ldqo=None, ldko=None, dtype=None, stream=None):
     """rot_dim: all of dim unless given.  norm: whether heads are normalised (weights None: by 1)."""
     _here(Q, K, wq, wk, positions, inv_freq, Qout, Kout)
+    _dense(torch.int32, positions)
+    _dense(torch.float32, inv_freq)
     ldq = heads * dim if ldq is None else ldq
     ldk = kv_heads * dim if ldk is None else ldk
-    _check(_lib.bwta_head_norm_rope(_ptr(Q), ldq, heads, _ptr(wq), _ptr(K), ldk, kv_heads, _ptr(wk), _dtype(K if Q is None else Q, dtype),
+    _check(_lib.bwta_head_norm_rope(_ptr(Q), ldq, heads, _ptr(wq), _ptr(K), ldk, kv_heads, _ptr(wk),
+                                    _dtype(dtype, *((K, wk, Kout) if Q is None else (Q, K, wq, wk, Qout, Kout))),
                                     M, dim, int(norm), eps, _ptr(positions), _ptr(inv_freq), dim if rot_dim is None else rot_dim, int(interleaved),
                                     _ptr(Qout), heads * dim if ldqo is None else ldqo, _ptr(Kout), kv_heads * dim if ldko is None else ldko,
                                     _stream(stream)))
 
 
 def _ldt(table, given):
+    if isinstance(table, torch.Tensor) and (table.dtype != torch.int32 or (table.dim() and table.stride(-1) != 1 and table.shape[-1] > 1)):
+        raise TypeError("a block table is int32, its rows without gaps, got %s of strides %s" % (table.dtype, tuple(table.stride())))
     if given is not None:
         return given
     return 0 if table is None or isinstance(table, int) else table.stride(0)
@@ -493,8 +515,9 @@ def _ldt(table, given):
 
 def _cache_rows(call, cache, K, V, table, lens, cu, M, batch, max_new, max_len, ldk, ldv, ldt, dtype, stream):
     _here(cache, K, V, table, lens, cu)
+    _dense(torch.int32, lens, cu)
     width = cache.kv_heads * cache.dim
-    _check(call(cache, _ptr(K), width if ldk is None else ldk, _ptr(V), width if ldv is None else ldv, _dtype(K, dtype), _ptr(table),
+    _check(call(cache, _ptr(K), width if ldk is None else ldk, _ptr(V), width if ldv is None else ldv, _dtype(dtype, K, V), _ptr(table),
                 _ldt(table, ldt), _ptr(lens), _ptr(cu), batch, M, max_new, max_len, _stream(stream)))
 
 
@@ -513,8 +536,10 @@ def cache_attention_workspace_bytes(*, M, heads, kv_heads, dim, batch, max_new, 
 def bwta_cache_attention(cache, Q, out, lse, table, lens, cu=None, workspace=None, *, M, batch, max_new, max_len, heads, alpha, causal=True, window=0,
                          ldq=None, ldo=None, ldt=None, dtype=None, workspace_bytes=None, stream=None):
     _here(cache, Q, out, lse, table, lens, cu, workspace)
+    _dense(torch.int32, lens, cu)
+    _dense(torch.float32, lse)
     width = heads * cache.dim
-    _check(_lib.bwta_cache_attention(cache, _ptr(Q), width if ldq is None else ldq, _ptr(out), width if ldo is None else ldo, _dtype(Q, dtype),
+    _check(_lib.bwta_cache_attention(cache, _ptr(Q), width if ldq is None else ldq, _ptr(out), width if ldo is None else ldo, _dtype(dtype, Q, out),
                                      _ptr(lse), _ptr(table), _ldt(table, ldt), _ptr(lens), _ptr(cu), batch, M, max_new, max_len, heads, alpha,
                                      int(causal), window, _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream)))
 

@@ -131,7 +131,33 @@ struct Here {
         if (t && t->get_device() != device) throw NotOrdinary{};
         return t;
     }
-    void *address(PyObject *o) const { return ::address(tensor(o)); }
+    // what binding._dtype and binding._dense refuse is theirs to refuse
+    const at::Tensor *rows(PyObject *o) const
+    {
+        const at::Tensor *t = tensor(o);
+        if (t && t->dim() && t->stride(-1) != 1 && t->size(-1) > 1) throw NotOrdinary{};
+        return t;
+    }
+    void *rows_like(PyObject *o, const at::Tensor *first) const
+    {
+        const at::Tensor *t = rows(o);
+        if (t && first && t->scalar_type() != first->scalar_type()) throw NotOrdinary{};
+        return ::address(t);
+    }
+    void *dense(PyObject *o, at::ScalarType type) const
+    {
+        const at::Tensor *t = tensor(o);
+        if (t && (t->scalar_type() != type || !t->is_contiguous())) throw NotOrdinary{};
+        return ::address(t);
+    }
+    int32_t *ints(PyObject *o) const { return (int32_t *)dense(o, at::kInt); }
+    float *floats(PyObject *o) const { return (float *)dense(o, at::kFloat); }
+    const at::Tensor *table(PyObject *o) const
+    {
+        const at::Tensor *t = rows(o);
+        if (t && t->scalar_type() != at::kInt) throw NotOrdinary{};
+        return t;
+    }
 };
 
 Here here(PyObject *stream)
@@ -365,18 +391,20 @@ bool matmul_bool_prepared(const Bound &b, PyObject *const *v, PyObject **result)
 bool head_norm_rope(const Bound &b, PyObject *const *v, PyObject **result)
 {
     const Here h = here(v[21]);
-    const at::Tensor *Q = h.tensor(v[0]), *K = h.tensor(v[1]);
+    const at::Tensor *Q = h.rows(v[0]), *K = h.rows(v[1]), *first = Q ? Q : K;
     const int M = int32(v[8]), heads = int32(v[9]), kv = int32(v[10]), dim = int32(v[11]), rot = (int)rows_apart(v[12], dim);
     if (given(v[12])) int32(v[12]);
     const float eps = number(v[13], 1e-6f);
     const int norm = flag(v[14], true), interleaved = flag(v[15], false);
     const int64_t wq = (int64_t)heads * dim, wk = (int64_t)kv * dim;
     const int64_t ldq = rows_apart(v[16], wq), ldk = rows_apart(v[17], wk), ldqo = rows_apart(v[18], wq), ldko = rows_apart(v[19], wk);
-    const int dtype = head_dtype(v[20], Q ? Q : K);
-    void *const pq = address(Q), *const pk = address(K), *const pwq = h.address(v[2]), *const pwk = h.address(v[3]), *const pos = h.address(v[4]),
-               *const freq = h.address(v[5]), *const qo = h.address(v[6]), *const ko = h.address(v[7]);
+    const int dtype = head_dtype(v[20], first);
+    void *const pq = address(Q), *const pk = h.rows_like(v[1], first), *const pwq = h.rows_like(v[2], first), *const pwk = h.rows_like(v[3], first),
+               *const qo = h.rows_like(v[6], first), *const ko = h.rows_like(v[7], first);
+    const int32_t *const pos = h.ints(v[4]);
+    const float *const freq = h.floats(v[5]);
     BWTA_FN(bwta_head_norm_rope);
-    return finish([&] { return call(pq, ldq, heads, pwq, pk, ldk, kv, pwk, dtype, M, dim, norm, eps, (const int32_t *)pos, (const float *)freq, rot, interleaved, qo, ldqo, ko, ldko, h.stream); }, result);
+    return finish([&] { return call(pq, ldq, heads, pwq, pk, ldk, kv, pwk, dtype, M, dim, norm, eps, pos, freq, rot, interleaved, qo, ldqo, ko, ldko, h.stream); }, result);
 }
 
 template <typename F>
@@ -384,14 +412,15 @@ bool cache_rows(F *call, PyObject *const *v, PyObject **result)
 {
     const Here h = here(v[14]);
     const Cache cache = cache_of(v[0], h);
-    const at::Tensor *K = h.tensor(v[1]), *table = h.tensor(v[3]);
+    const at::Tensor *K = h.rows(v[1]), *table = h.table(v[3]);
     const int M = int32(v[6]), batch = int32(v[7]), max_new = int32(v[8]), max_len = int32(v[9]);
     const int64_t width = (int64_t)cache.c.kv_heads * cache.c.dim, ldk = rows_apart(v[10], width), ldv = rows_apart(v[11], width);
     if (!given(v[12]) && (!table || table->dim() == 0)) throw NotOrdinary{};
     const int64_t ldt = rows_apart(v[12], table ? table->stride(0) : 0);
     const int dtype = head_dtype(v[13], K);
-    void *const pk = address(K), *const pv = h.address(v[2]), *const pt = address(table), *const lens = h.address(v[4]), *const cu = h.address(v[5]);
-    return finish([&] { return call(&cache.c, pk, ldk, pv, ldv, dtype, (const int32_t *)pt, ldt, (const int32_t *)lens, (const int32_t *)cu, batch, M, max_new, max_len, h.stream); }, result);
+    void *const pk = address(K), *const pv = h.rows_like(v[2], K), *const pt = address(table);
+    const int32_t *const lens = h.ints(v[4]), *const cu = h.ints(v[5]);
+    return finish([&] { return call(&cache.c, pk, ldk, pv, ldv, dtype, (const int32_t *)pt, ldt, lens, cu, batch, M, max_new, max_len, h.stream); }, result);
 }
 
 bool cache_write(const Bound &b, PyObject *const *v, PyObject **result)
@@ -410,7 +439,7 @@ bool cache_attention(const Bound &b, PyObject *const *v, PyObject **result)
 {
     const Here h = here(v[21]);
     const Cache cache = cache_of(v[0], h);
-    const at::Tensor *Q = h.tensor(v[1]), *table = h.tensor(v[4]), *ws = h.tensor(v[7]);
+    const at::Tensor *Q = h.rows(v[1]), *table = h.table(v[4]), *ws = h.tensor(v[7]);
     const int M = int32(v[8]), batch = int32(v[9]), max_new = int32(v[10]), max_len = int32(v[11]), heads = int32(v[12]);
     if (!v[13]) throw NotOrdinary{};
     const float alpha = number(v[13], 0.0f);
@@ -420,10 +449,11 @@ bool cache_attention(const Bound &b, PyObject *const *v, PyObject **result)
     const int64_t ldt = rows_apart(v[18], table ? table->stride(0) : 0);
     const int dtype = head_dtype(v[19], Q);
     const size_t bytes = bytes_of(v[20], ws);
-    void *const pq = address(Q), *const po = h.address(v[2]), *const lse = h.address(v[3]), *const pt = address(table), *const lens = h.address(v[5]),
-               *const cu = h.address(v[6]), *const pws = address(ws);
+    void *const pq = address(Q), *const po = h.rows_like(v[2], Q), *const pt = address(table), *const pws = address(ws);
+    float *const lse = h.floats(v[3]);
+    const int32_t *const lens = h.ints(v[5]), *const cu = h.ints(v[6]);
     BWTA_FN(bwta_cache_attention);
-    return finish([&] { return call(&cache.c, pq, ldq, po, ldo, dtype, (float *)lse, (const int32_t *)pt, ldt, (const int32_t *)lens, (const int32_t *)cu, batch, M, max_new, max_len,
+    return finish([&] { return call(&cache.c, pq, ldq, po, ldo, dtype, lse, (const int32_t *)pt, ldt, lens, cu, batch, M, max_new, max_len,
                                     heads, alpha, causal, window, pws, bytes, h.stream); }, result);
 }
 

@@ -626,6 +626,7 @@ int bwta_cache_write(const bwta_cache *cache, const void *K, int64_t ldk, const 
     bool none;
     int rc = check_cache_call(cache, dtype, table, ldt, lens, cu, batch, M, max_new, max_len, &none);
     if (rc != BWTA_OK || none) return rc;
+    max_new = max_new < M ? max_new : M;  // no sequence has more
     const bwta::SeqArgs s{table, ldt, lens, cu, batch, M, max_new, max_len};
     if ((rc = check_cache_rows(cache, K, ldk, V, ldv, s))) return rc;
     return hip_result(bwta::launch_cache_write({cache_args(cache), s, K, V, ldk, ldv, dtype == BWTA_DTYPE_BF16}, (hipStream_t)stream));
@@ -638,6 +639,7 @@ int bwta_cache_read(const bwta_cache *cache, void *K, int64_t ldk, void *V, int6
     bool none;
     int rc = check_cache_call(cache, dtype, table, ldt, lens, cu, batch, M, max_new, max_len, &none);
     if (rc != BWTA_OK || none) return rc;
+    max_new = max_new < M ? max_new : M;  // no sequence has more
     const bwta::SeqArgs s{table, ldt, lens, cu, batch, M, max_new, max_len};
     if ((rc = check_cache_rows(cache, K, ldk, V, ldv, s))) return rc;
     if (rows_clash(K, ldk, cache->kv_heads, V, ldv, cache->kv_heads, M, cache->dim, false)) return BWTA_ERR_UNSUPPORTED;
@@ -647,7 +649,7 @@ int bwta_cache_read(const bwta_cache *cache, void *K, int64_t ldk, void *V, int6
 size_t bwta_cache_attention_workspace_bytes(int M, int heads, int kv_heads, int dim, int batch, int max_new, int max_len)
 {
     if (M <= 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || heads > kMostHeads || dim <= 0 || dim > 256 || batch <= 0 || max_new <= 0 || max_len <= 0) return 0;
-    return round_up(bwta::cache_attention_plan(heads, kv_heads, dim, batch, max_new, max_len).workspace, 256);
+    return round_up(bwta::cache_attention_plan(heads, kv_heads, dim, batch, max_new < M ? max_new : M, max_len).workspace, 256);
 }
 
 int bwta_cache_attention(const bwta_cache *cache, const void *Q, int64_t ldq, void *out, int64_t ldo, int dtype, float *lse,
@@ -669,6 +671,7 @@ int bwta_cache_attention(const bwta_cache *cache, const void *Q, int64_t ldq, vo
     const size_t need = bwta_cache_attention_workspace_bytes(M, heads, cache->kv_heads, cache->dim, batch, max_new, max_len);
     if (need && (!workspace || workspace_bytes < need)) return BWTA_ERR_WORKSPACE;
     if (need && !aligned(workspace, 256)) return BWTA_ERR_ALIGN;
+    max_new = max_new < M ? max_new : M;  // no sequence has more
     const bwta::SeqArgs s{table, ldt, lens, cu, batch, M, max_new, max_len};
     bwta::AttentionPlan plan = bwta::cache_attention_plan(heads, cache->kv_heads, cache->dim, batch, max_new, max_len);
     const int64_t reach = (int64_t)window + max_new + 62;  // the workspace is for any window, so a plan for this one has to fit it

@@ -560,3 +560,14 @@ def test_many_rows_in_short_parts(dim, heads, kv, lens, new, dtype):
     """Parts of four steps and more, up to one round of workgroups."""
     case(91 + dim, lens, new, heads, kv, 64, dim, dtype)
     case(92 + dim, lens, new, heads, kv, 64, dim, dtype, False)
+
+
+def test_bounds_above_the_number_of_rows():
+    """max_new counts as M where it is larger: the same layout of the work, the same workspace."""
+    g = torch.Generator().manual_seed(97)
+    lens, new = [3000, 500], [1, 2]
+    ref, table = filled(g, lens, 2, 64, 128)
+    Q = torch.randn((3, 4, 128), generator=g).half()
+    a, b = (run(ref, ref.device(B), Q, table, lens, new, 4, 0.1, True, 0, max_new=n) for n in (3, 1 << 30))
+    check(ref, Q, table, lens, new, 4, 0.1, True, 0, a)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])

@@ -96,3 +96,24 @@ def test_other_forms_are_the_python_forms():
         a[i] = a[i].float()
         with pytest.raises(TypeError):
             getattr(B, name)(*a, **kw)
+
+
+def test_tensors_of_other_types_or_strides_are_refused():
+    """Whoever marshals: 64-bit lengths, rows of two types, elements apart, a table's columns."""
+    for name, make, kw, written in _calls(torch.float16):
+        for i, x in enumerate(make()):
+            if not isinstance(x, torch.Tensor) or (name == "bwta_cache_attention" and i == 7):
+                continue
+            bad = [x.double() if x.is_floating_point() else x.long()]
+            if x.numel() > 1:
+                bad.append(torch.stack([x, x], dim=-1)[..., 0])
+            if x.dtype == torch.float16 and i != (1 if name.startswith("bwta_cache") else 0):
+                bad.append(x.bfloat16())
+            for y in bad:
+                a = make()
+                a[i] = y
+                before = [a[j].clone() for j in written if isinstance(a[j], torch.Tensor)]
+                with pytest.raises((TypeError, ValueError)):
+                    getattr(B, name)(*a, **kw)
+                torch.cuda.synchronize()
+                assert all(torch.equal(b, a[j]) for b, j in zip(before, [j for j in written if isinstance(a[j], torch.Tensor)]))
