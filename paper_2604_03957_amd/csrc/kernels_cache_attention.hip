@@ -402,16 +402,9 @@ __global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_c
 template <int CHUNKS>
 __device__ __forceinline__ constexpr int padded(int row, int chunk) { return row * (CHUNKS + 1) + chunk; }
 
-// Many rows: each wavefront has 32 of its own, and four wavefronts share the keys and values of a step, which reach LDS as
-// 16-bit numbers (each code is widened once for the four).  Products of 32 x 32: key row 8 i + 4 j + r of a block of 32 is
-// token 16 j + 4 i + r, so a lane again has 16 tokens in a row.
-// A turn computes the scores of the next step beside the weights and the sums of this one: matrix cores and vector ALU have
-// work that does not wait for each other's.  Keys are therefore fetched one step before values.
-// Workgroups that share all steps equally (share_log2 >= 0) go through those of a sequence's first head's first 128 rows, second
-// 128 and so on, next head, next sequence; what begins or ends inside somebody else's share becomes a part, and each leaves
-// where it begins for the join.
+// What one tile of 128 rows of a sequence and key head sees.
 struct RowsReach {
-    int step0, steps, units;  // as Reach's, of the rows of one tile
+    int step0, steps, units;  // as Reach's
 };
 constexpr int kTileRows = 128, kMostShared = 1024;  // tiles that are shared at most (sequences, too: a workgroup counts each one's steps)
 __device__ __forceinline__ RowsReach rows_reach(const CacheAttentionArgs &a, const Seq &s, int group, int total, int tile)
@@ -428,8 +421,16 @@ __device__ __forceinline__ RowsReach rows_reach(const CacheAttentionArgs &a, con
 // where each sharing workgroup begins, behind the parts: sequence (-1: nowhere), head, tile, steps of the tile before it
 __device__ __forceinline__ int4 *begins_of(const CacheAttentionArgs &a) { return (int4 *)(a.partial + a.part_rows * (a.cache.dim + 2)); }
 
+// Many rows: each wavefront has 32 of its own, and four wavefronts share the keys and values of a step, which reach LDS as
+// 16-bit numbers (each code is widened once for the four).  Products of 32 x 32: key row 8 i + 4 j + r of a block of 32 is
+// token 16 j + 4 i + r, so a lane again has 16 tokens in a row.
+// A turn computes the scores of the next step beside the weights and the sums of this one: matrix cores and vector ALU have
+// work that does not wait for each other's.  Keys are therefore fetched one step before values.
 // With GROUPS = 2 a workgroup has the rows twice: one four take the even steps, the other the odd ones, and their sums are
 // joined through LDS.
+// With SHARES workgroups share all steps equally: those of a sequence's first head's first 128 rows, second 128 and so on, next
+// head, next sequence.  What begins or ends inside somebody else's share becomes a part, and each leaves where it begins for
+// the join.
 // Bound by issue: a step of 32 rows is 1024 cycles of matrix cores beside some 1000 of vector ALU (32 weights a lane with a
 // fused multiply-add, a power, an addition and half a conversion each, and the widening), and 32 KB from LDS a wavefront.
 // 8192 keys for each of 2048 rows, 32 heads of 128: 920 TFLOP/s with two groups and 970 with one, where a large fp16 product
@@ -786,7 +787,10 @@ __global__ __launch_bounds__(GROUPS * 256, D <= 128 ? 2 : 1) void k_cache_attent
         }
         if (has && !side) {
             int64_t part = part0 + wave * R + q32;
-            if (part0 < 0) part = a.splits > 1 ? ((int64_t)(blockIdx.x % a.splits) * a.seq.batch + b) * a.seq.max_new * a.heads + (int64_t)token * a.heads + head * group + row - token * group : -1;
+            if (part0 < 0) {
+                const int64_t first_row = ((int64_t)(blockIdx.x % a.splits) * a.seq.batch + b) * a.seq.max_new;
+                part = a.splits > 1 ? (first_row + token) * a.heads + head * group + row - token * group : -1;
+            }
 #pragma unroll
             for (int n = 0; n < DN; ++n)
 #pragma unroll
@@ -965,11 +969,9 @@ void launch(const CacheAttentionArgs &a, const AttentionPlan &plan, hipStream_t 
     const dim3 grid((unsigned)plan.groups), block(kAttWaves * 64);
     if (plan.rows > 32) {
         // Two workgroups' worth of wavefronts on the same rows halve the way of the rows that see most, which is what few
-        // workgroups take their time for; many balance by themselves, unless long sequences of a batch differ.  us, one / two,
-        // heads of 128: a causal prompt of 2048 with 32 heads 58 / 55, two of them 95 / 109; 128 rows over 256 keys, 32 times,
-        // 40 / 56; chunks of up to 1024 tokens over 5163 to 16024 keys, four times, 641 / 610.
+        // workgroups take their time for; many balance by themselves.  us, one / two, heads of 128: a causal prompt of 2048 with 32
+        // heads 58 / 55, two of them 95 / 109; 128 rows over 256 keys, 32 times, 40 / 56.
         constexpr int kMost = D <= 128 ? 2 : 1;
-        const bool differ = a.seq.batch > 1 && plan.reach >= 8192;
         if constexpr (D <= 128) {
             if (a.share_log2 >= 0) {
                 hipLaunchKernelGGL((k_cache_attention_rows<T, D, 1, true>), grid, block, 0, st, a, plan.row_tiles);
@@ -977,7 +979,7 @@ void launch(const CacheAttentionArgs &a, const AttentionPlan &plan, hipStream_t 
                 return;
             }
         }
-        if (kMost == 2 && plan.reach >= 1024 && plan.groups <= (differ ? 1024 : 512))
+        if (kMost == 2 && plan.reach >= 1024 && plan.groups <= 512)
             hipLaunchKernelGGL((k_cache_attention_rows<T, D, kMost, false>), grid, dim3(kMost * 256), 0, st, a, plan.row_tiles);
         else
             hipLaunchKernelGGL((k_cache_attention_rows<T, D, 1, false>), grid, block, 0, st, a, plan.row_tiles);
@@ -1029,7 +1031,7 @@ AttentionPlan cache_attention_plan(int heads, int kv_heads, int dim, int batch, 
                 // twice the wavefronts, which join in LDS (32 sequences of 2048 keys, 8 heads of 128: 24.5 us, two parts 27.6;
                 // 512 keys, one sequence: 7.4 and 8.8); heads of 256 have no registers for that
                 p.waves = 2 * kAttWaves;
-            } else if (splits > 2) {
+            } else if (splits > 1) {
                 p.splits = (int)splits;
                 p.groups *= (double)splits;
                 p.part_rows = (int64_t)p.groups * p.rows;
@@ -1053,7 +1055,8 @@ AttentionPlan cache_attention_plan(int heads, int kv_heads, int dim, int batch, 
     // and 5163 to 16024, four times, 595 / 532.  Against that 512 and 32768 keys four times 1131 / 1154, 512 and 2048 four times
     // 78 / 95, a prompt of 8192 572 / 615, 2048 and 32768 four times 4292 / 4950; heads of 256 lose registers.
     const double all = p.groups * (double)steps, rounds = p.groups / 256, fill = rounds / (double)(int64_t)(rounds + 255.0 / 256);
-    if (dim < 256 && steps >= 64 && p.groups > 256 && p.groups <= kMostShared && (int64_t)max_new * 2 <= reach && (batch > 1 || fill < 0.85) && all < (double)(1u << 31)) {
+    const bool few_rounds = p.groups > 256 && p.groups <= kMostShared, uneven = batch > 1 || fill < 0.85;
+    if (dim < 256 && steps >= 64 && few_rounds && uneven && (int64_t)max_new * 2 <= reach && all < (double)(1u << 31)) {
         p.share_log2 = 9;
         p.groups = 1 << p.share_log2;
         p.part_rows = (int64_t)2 * kTileRows << p.share_log2;
