@@ -293,8 +293,9 @@ __global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_c
             }
 
             const float c = fmaxf(a.alpha * kLog2e * x.ks, 1.17549435e-38f);
-            const int ev = __builtin_amdgcn_readfirstlane(exponent_of(x.vs));
-            if (!begun) eref = ev, begun = true;
+            // (a block that is not there has no scale: what memory holds in its place decides nothing)
+            const int ev = x.ok ? __builtin_amdgcn_readfirstlane(exponent_of(x.vs)) : eref;
+            if (x.ok && !begun) eref = ev, begun = true;
             if (ev - eref > kDrift || eref - ev > kDrift) {
                 const float f = pow2(eref - ev);
                 eref = ev;
@@ -561,6 +562,7 @@ __global__ __launch_bounds__(GROUPS * 256, D <= 128 ? 2 : 1) void k_cache_attent
         float16v o[DN] = {};
         float m = -INFINITY, l = 0.0f, top = -INFINITY;
         int eref = 0;
+        bool begun = false;
         const int block_shift = a.cache.block >> 7;  // 64, 128, 256 tokens: 1, 2, 4 steps
 
         // Loads run ahead of what waits for them.  Steps behind the last are the last again, but that nobody sees it, so that
@@ -674,7 +676,6 @@ __global__ __launch_bounds__(GROUPS * 256, D <= 128 ? 2 : 1) void k_cache_attent
                 for (int kk = 0; kk < KK; ++kk) score(0, kb, kk);
             hide(s0);
             top = largest();
-            eref = __builtin_amdgcn_readfirstlane(exponent_of(s0.vs));
 
             // one step; the last one looks at none behind it
             auto take = [&](int turn, auto last) {
@@ -689,7 +690,9 @@ __global__ __launch_bounds__(GROUPS * 256, D <= 128 ? 2 : 1) void k_cache_attent
                 }
 
                 const float c = fmaxf(a.alpha * kLog2e * s0.ks, 1.17549435e-38f);
-                const int ev = __builtin_amdgcn_readfirstlane(exponent_of(s0.vs));
+                // (a block that is not there has no scale: what memory holds in its place decides nothing)
+                const int ev = s0.ok ? __builtin_amdgcn_readfirstlane(exponent_of(s0.vs)) : eref;
+                if (s0.ok && !begun) eref = ev, begun = true;
                 if (ev - eref > kDrift || eref - ev > kDrift) {
                     const float f = pow2(eref - ev);
                     eref = ev;
