@@ -384,7 +384,7 @@ int bwta_cache_read(const bwta_cache *cache, void *K, int64_t ldk, void *V, int6
  * tokens up to p (itself among them: write first, then attend), with window > 0 of these the last
  * `window`; with causal == 0 all lens[b] tokens (an encoder's states: then the rows need not be in the
  * cache).  Tokens of blocks that are not there are not seen.  A row that sees nothing gets 0, and -Inf
- * in lse.
+ * in lse.  Beyond dtype's range a result is its largest, as in reading.
  *   heads    a multiple of the cache's kv_heads
  *   alpha    finite and > 0; window >= 0, and 0 unless causal (BWTA_ERR_UNSUPPORTED)
  *   out      [M, heads, dim] in dtype; may be Q itself (same address and ld), must not overlap it else

@@ -90,6 +90,15 @@ __device__ __forceinline__ Reach reach(const CacheAttentionArgs &a, const Seq &s
     return r;
 }
 
+// Four channels of a result.  Averages of finite values stay finite: a code may stand for more than fp16 has (65504 is held as
+// 256 * 2^8, infinities as 448 * 2^e), and what is beyond the type's range is its largest, as in reading.
+template <typename T>
+__device__ __forceinline__ uint2 result(float4v x, float f)
+{
+    auto fit = [&](float y) { return y * f != y * f ? y * f : fminf(fmaxf(y * f, -Half<T>::kMax), Half<T>::kMax); };  // (a NaN stays one)
+    return make_uint2(Half<T>::pack(fit(x[0]), fit(x[1])), Half<T>::pack(fit(x[2]), fit(x[3])));
+}
+
 // Four channels of a row, and once per row its maximum (as a power of two) and sum: the result, or the part of it that
 // `part` says is kept for the join.
 template <typename T, int D>
@@ -103,7 +112,7 @@ __device__ __forceinline__ void give(const CacheAttentionArgs &a, const Seq &s, 
     const int t = (unsigned)row / (unsigned)group, h = head * group + (row - t * group);
     const int64_t token = s.row + t;
     const float f = l == 0.0f ? 0.0f : 1.0f / l;
-    *(uint2 *)((T *)a.out + token * a.ldo + (int64_t)h * D + channel) = make_uint2(Half<T>::pack(x[0] * f, x[1] * f), Half<T>::pack(x[2] * f, x[3] * f));
+    *(uint2 *)((T *)a.out + token * a.ldo + (int64_t)h * D + channel) = result<T>(x, f);
     if (once && a.lse) a.lse[token * a.heads + h] = kLn2 * (m + log2f(l));
 }
 
@@ -959,7 +968,7 @@ __global__ __launch_bounds__(256) void k_cache_attention_join(CacheAttentionArgs
     }
     const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
     const int64_t token = s.row + t;
-    *(uint2 *)((T *)a.out + token * a.ldo + (int64_t)h * D + 4 * c) = make_uint2(Half<T>::pack(x[0] * f, x[1] * f), Half<T>::pack(x[2] * f, x[3] * f));
+    *(uint2 *)((T *)a.out + token * a.ldo + (int64_t)h * D + 4 * c) = result<T>(x, f);
     if (c == 0 && a.lse) a.lse[token * a.heads + h] = kLn2 * (top + log2f(sum));
 }
 
