@@ -298,7 +298,8 @@ int bwta_prepare_act_autoscale(const void *A, int64_t lda, int M, int K, void *s
  * bwta_linear writes, or a part of them (heads of a fused q/k/v projection).  Rows start at 16-byte
  * aligned addresses and ld is a multiple of 8 (BWTA_ERR_ALIGN).  Up to 16384 heads
  * and, rotated, 2^25 tokens (BWTA_ERR_TOO_LARGE).
- * Computation is in fp32, each result is rounded once to dtype.
+ * Computation is in fp32, each result is rounded once to dtype (one exception: the weights of
+ * bwta_cache_attention, see there).
  */
 
 /*
@@ -384,7 +385,9 @@ int bwta_cache_read(const bwta_cache *cache, void *K, int64_t ldk, void *V, int6
  * tokens up to p (itself among them: write first, then attend), with window > 0 of these the last
  * `window`; with causal == 0 all lens[b] tokens (an encoder's states: then the rows need not be in the
  * cache).  Tokens of blocks that are not there are not seen.  A row that sees nothing gets 0, and -Inf
- * in lse.  Beyond dtype's range a result is its largest, as in reading.
+ * in lse.  Beyond dtype's range a result is its largest, as in reading.  Scores, p's denominator, lse and
+ * all sums are fp32; the p_j that multiply values are rounded to fp16: each, times its value's scale, is off by
+ * at most 2^-11 of itself or 2^-36 of the row's largest, whichever is more.
  *   heads    a multiple of the cache's kv_heads
  *   alpha    finite and > 0; window >= 0, and 0 unless causal (BWTA_ERR_UNSUPPORTED)
  *   out      [M, heads, dim] in dtype; may be Q itself (same address and ld), must not overlap it else

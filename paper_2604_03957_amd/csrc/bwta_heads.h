@@ -168,7 +168,7 @@ struct CacheAttentionArgs {
     float alpha;
     bool causal, bf16;
     int window;
-    // Parts of rows that are joined afterwards: [part_rows][dim] sums, then [part_rows][2] maximum and sum of weights.  Many
+    // Parts of rows that are joined afterwards: [part_rows][dim] sums, then [part_rows][2] m and sum of weights.  Many
     // rows: [splits][batch * max_new * heads].  Few (share_rows of them a workgroup): [batch * key heads][splits][share_rows], or where
     // 2^share_log2 workgroups share all steps (-1: they do not) [workgroups][2][share_rows], and behind the parts how many
     // steps lie before each sequence.

@@ -1,11 +1,13 @@
 // Attention of 16-bit queries over the 8-bit cache, in one pass over the keys:
-//   out = sum_j p_j v_j / sum_j p_j,   p_j = exp(alpha q . k_j - m),   m a running maximum
-// with sums, maximum and scores in fp32.
+//   out = sum_j p_j v_j / sum_j p_j,   p_j = 2^(s_j - m),   s_j = alpha log2(e) q . k_j,   m near a running maximum
+// with sums and scores in fp32.
 //
 // Codes are exact in both 16-bit types, so q . k is the matrix cores' sum of exact products; a block's key scale joins
-// alpha.  Weights are rounded to fp16 for the second product whatever the queries' type: they lie in [0, 2^12], where
-// fp16 has 11 bits to bf16's 8.  Value codes enter without their scale; sums are kept in units of 2^eref, the scale of
-// some block, and the few bits between that and the block at hand go into the weights' exponent.
+// alpha.  Value codes enter without their scale 2^e, which joins the weights: s_j + e - m is the exponent of what the second
+// product takes, rounded to fp16 whatever the queries' type (11 bits to bf16's 8).  m is moved when an exponent exceeds 15, so
+// that it becomes 11: the upper end of fp16's range.  A weight times scale is then off by at most 2^-11 of itself, or 2^-25 where
+// the row's largest is 2^11 or more, 2^-36 of that, which is less than sums in fp32 lose.  What m was moved for last is
+// exactly 2^11, so a row that one key rules does not feel the rounding; and the log-sum-exp sums the weights in fp32.
 //
 // The first product is computed transposed, keys by queries: its result has a query per
 // lane and, with the key rows taken in the right order (row 4 i + r of the b-th 16 is token 16 i + 4 b + r), 16 tokens in
@@ -53,8 +55,11 @@ __device__ __forceinline__ typename Mma<T>::Frag widen(uint32_t lo, uint32_t hi)
 }
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
-constexpr float kSlack = 8.0f;  // weights may reach 2^kSlack before the maximum is moved
-constexpr int kDrift = 4;       // bits a block's value scale may differ from eref
+
+constexpr float kHighest = 15.0f, kPlace = 11.0f;  // exponents of weights: where m has to move, and what the moved one leaves
+constexpr float kNothing = -3e38f;                  // m before any key has been seen
+// m for keys of which the largest has exponent e.  (As it was for a NaN, and for the -Inf of keys that are not seen.)
+__device__ __forceinline__ float moved(float e, float m) { return e > m + kHighest ? e - kPlace : m; }
 
 // The larger one; a NaN if either is one (which saves making a quiet one of it first).
 __device__ __forceinline__ float most(float x, float y) { return __builtin_elementwise_maximum(x, y); }
@@ -99,7 +104,7 @@ __device__ __forceinline__ uint2 result(float4v x, float f)
     return make_uint2(Half<T>::pack(fit(x[0]), fit(x[1])), Half<T>::pack(fit(x[2]), fit(x[3])));
 }
 
-// Four channels of a row, and once per row its maximum (as a power of two) and sum: the result, or the part of it that
+// Four channels of a row, and once per row its m and sum: the result, or the part of it that
 // `part` says is kept for the join.
 template <typename T, int D>
 __device__ __forceinline__ void give(const CacheAttentionArgs &a, const Seq &s, int head, int group, int64_t part, int row, int channel, float4v x, float m, float l, bool once)
@@ -155,7 +160,7 @@ __global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_c
         if (a.splits > 1) part = blockIdx.x;
         if (left == 0) {  // fewer steps than splits: nothing to add
             for (int at = threadIdx.x; at < see.rows * (D / 4); at += WAVES * 64)
-                give<T, D>(a, s, 0, 1, part * R + at / (D / 4), 0, at % (D / 4) * 4, float4v{}, -INFINITY, 0.0f, at % (D / 4) == 0);
+                give<T, D>(a, s, 0, 1, part * R + at / (D / 4), 0, at % (D / 4) * 4, float4v{}, kNothing, 0.0f, at % (D / 4) == 0);
             return;
         }
     } else {
@@ -258,9 +263,7 @@ __global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_c
         float4v o[NB][NV] = {};
         float m[NB], l[NB];
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) m[nb] = -INFINITY, l[nb] = 0.0f;
-        int eref = 0;
-        bool begun = false;
+        for (int nb = 0; nb < NB; ++nb) m[nb] = kNothing, l[nb] = 0.0f;
         auto compute = [&](Turn &x, int step) {
             float4v sc[NB][4] = {};
 #pragma unroll
@@ -303,33 +306,23 @@ __global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_c
 
             const float c = fmaxf(a.alpha * kLog2e * x.ks, 1.17549435e-38f);
             // (a block that is not there has no scale: what memory holds in its place decides nothing)
-            const int ev = x.ok ? __builtin_amdgcn_readfirstlane(exponent_of(x.vs)) : eref;
-            if (x.ok && !begun) eref = ev, begun = true;
-            if (ev - eref > kDrift || eref - ev > kDrift) {
-                const float f = pow2(eref - ev);
-                eref = ev;
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-                    for (int n = 0; n < NV; ++n) o[nb][n] *= f;
-            }
-            const float drift = (float)(ev - eref), undrift = pow2(eref - ev);
+            const int ev = x.ok ? __builtin_amdgcn_readfirstlane(exponent_of(x.vs)) : 0;
             half8 p[NB][2];
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
                 float top = most(most(sc[nb][0][0], sc[nb][0][1]), most(sc[nb][0][2], sc[nb][0][3]));
 #pragma unroll
                 for (int kb = 1; kb < 4; ++kb) top = most(most(top, most(sc[nb][kb][0], sc[nb][kb][1])), most(sc[nb][kb][2], sc[nb][kb][3]));
-                top *= c;
-                if (__any(top > m[nb] + kSlack)) {
-                    const float now = fmaxf(m[nb], max_of_query(top));
-                    const float f = m[nb] == -INFINITY ? 0.0f : exp2f(m[nb] - now);
-                    m[nb] = now;
+                top = fmaf(top, c, (float)ev);
+                if (__any(top > m[nb] + kHighest)) {
+                    const float to = moved(max_of_query(top), m[nb]);
+                    const float f = exp2f(m[nb] - to);
+                    m[nb] = to;
                     l[nb] *= f;
 #pragma unroll
                     for (int n = 0; n < NV; ++n) o[nb][n] *= f;
                 }
-                const float base = (m[nb] == -INFINITY ? 0.0f : m[nb]) - drift;
+                const float base = m[nb] - (float)ev;
                 float sum = 0.0f, w[16];
 #pragma unroll
                 for (int kb = 0; kb < 4; ++kb)
@@ -338,11 +331,11 @@ __global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_c
                         w[4 * kb + r] = __builtin_amdgcn_exp2f(fmaf(sc[nb][kb][r], c, -base));
                         sum += w[4 * kb + r];
                     }
-                l[nb] = fmaf(sum, undrift, l[nb]);
 #pragma unroll
                 for (int hf = 0; hf < 2; ++hf)
                     p[nb][hf] = half8{(_Float16)w[8 * hf], (_Float16)w[8 * hf + 1], (_Float16)w[8 * hf + 2], (_Float16)w[8 * hf + 3],
                                       (_Float16)w[8 * hf + 4], (_Float16)w[8 * hf + 5], (_Float16)w[8 * hf + 6], (_Float16)w[8 * hf + 7]};
+                l[nb] = fmaf(sum, pow2(-ev), l[nb]);  // the sum of weights alone knows no value's scale
             }
 #pragma unroll
             for (int n = 0; n < NV; ++n) {
@@ -359,14 +352,9 @@ __global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_c
             compute(turn, step);
         }
 
-        // o[nb][n][r]: query q16 of the nb-th 16, channel 16 n + 4 g + r, in units of 2^eref
-        const float unit = pow2(eref);
+        // o[nb][n][r]: query q16 of the nb-th 16, channel 16 n + 4 g + r
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            l[nb] = sum_of_query(l[nb]);
-#pragma unroll
-            for (int n = 0; n < NV; ++n) o[nb][n] *= unit;
-        }
+        for (int nb = 0; nb < NB; ++nb) l[nb] = sum_of_query(l[nb]);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             const int at = wave * R + nb * 16 + q16;
@@ -378,14 +366,14 @@ __global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_c
         for (int at = threadIdx.x; at < R * (D / 4); at += WAVES * 64) {
             const int r = at / (D / 4);
             if (r >= total) continue;
-            float top = -INFINITY, sum = 0.0f;
+            float top = kNothing, sum = 0.0f;
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) top = fmaxf(top, merged_ml[w * R + r].x);
             float4v x = {};
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) {
                 const float2 ml = merged_ml[w * R + r];
-                const float f = ml.x == -INFINITY && ml.y == 0.0f ? 0.0f : exp2f(ml.x - top);  // a NaN among the scores stays one
+                const float f = exp2f(ml.x - top);
                 const float4 y = merged[w * R * (D / 4) + at];
                 x += float4v{y.x, y.y, y.z, y.w} * f;
                 sum = fmaf(ml.y, f, sum);
@@ -569,9 +557,7 @@ __global__ __launch_bounds__(GROUPS * 256, D <= 128 ? 2 : 1) void k_cache_attent
         }
 
         float16v o[DN] = {};
-        float m = -INFINITY, l = 0.0f, top = -INFINITY;
-        int eref = 0;
-        bool begun = false;
+        float m = kNothing, l = 0.0f, top = kNothing;
         const int block_shift = a.cache.block >> 7;  // 64, 128, 256 tokens: 1, 2, 4 steps
 
         // Loads run ahead of what waits for them.  Steps behind the last are the last again, but that nobody sees it, so that
@@ -700,25 +686,17 @@ __global__ __launch_bounds__(GROUPS * 256, D <= 128 ? 2 : 1) void k_cache_attent
 
                 const float c = fmaxf(a.alpha * kLog2e * s0.ks, 1.17549435e-38f);
                 // (a block that is not there has no scale: what memory holds in its place decides nothing)
-                const int ev = s0.ok ? __builtin_amdgcn_readfirstlane(exponent_of(s0.vs)) : eref;
-                if (s0.ok && !begun) eref = ev, begun = true;
-                if (ev - eref > kDrift || eref - ev > kDrift) {
-                    const float f = pow2(eref - ev);
-                    eref = ev;
-#pragma unroll
-                    for (int n = 0; n < DN; ++n) o[n] *= f;
-                }
-                const float drift = (float)(ev - eref), undrift = pow2(eref - ev);
-                top *= c;
-                if (__any(top > m + kSlack)) {
-                    const float up = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)));
-                    const float f = m == -INFINITY ? 0.0f : exp2f(m - up);
-                    m = up;
+                const int ev = s0.ok ? __builtin_amdgcn_readfirstlane(exponent_of(s0.vs)) : 0;
+                top = fmaf(top, c, (float)ev);
+                if (__any(top > m + kHighest)) {
+                    const float to = moved(fmaxf(top, __shfl_xor(top, 32)), m);
+                    const float f = exp2f(m - to);
+                    m = to;
                     l *= f;
 #pragma unroll
                     for (int n = 0; n < DN; ++n) o[n] *= f;
                 }
-                const float base = (m == -INFINITY ? 0.0f : m) - drift;
+                const float base = m - (float)ev;
                 now[0] = ahead[0], now[1] = ahead[1];
 
                 float sum[4] = {};
@@ -748,7 +726,7 @@ __global__ __launch_bounds__(GROUPS * 256, D <= 128 ? 2 : 1) void k_cache_attent
                 for (int t = 0; t < 4; ++t)
 #pragma unroll
                     for (int n = 0; n < DN; ++n) gather(n, t);
-                l = fmaf((sum[0] + sum[1]) + (sum[2] + sum[3]), undrift, l);
+                l = fmaf((sum[0] + sum[1]) + (sum[2] + sum[3]), pow2(-ev), l);  // the sum of weights alone knows no value's scale
                 if constexpr (!last.value) {
                     hide(s1);
                     top = largest();
@@ -762,14 +740,13 @@ __global__ __launch_bounds__(GROUPS * 256, D <= 128 ? 2 : 1) void k_cache_attent
             take(turn, std::true_type{});
         }
 
-        // o[n][r]: query q32, channel 32 n + 8 (r / 4) + 4 h2 + r % 4, in units of 2^eref
-        const float unit = pow2(eref);
+        // o[n][r]: query q32, channel 32 n + 8 (r / 4) + 4 h2 + r % 4
         float4v x[DN][4];
         l += __shfl_xor(l, 32);
 #pragma unroll
         for (int n = 0; n < DN; ++n)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) x[n][r] = float4v{o[n][4 * r], o[n][4 * r + 1], o[n][4 * r + 2], o[n][4 * r + 3]} * unit;
+            for (int r = 0; r < 4; ++r) x[n][r] = float4v{o[n][4 * r], o[n][4 * r + 1], o[n][4 * r + 2], o[n][4 * r + 3]};
         if constexpr (GROUPS == 2) {
             constexpr int kSums = DN * 4 * NT;
             static_assert(sizeof(tiles) >= kSums * sizeof(float4v) + NT * sizeof(float2), "the sums go where keys and values were");
@@ -787,8 +764,7 @@ __global__ __launch_bounds__(GROUPS * 256, D <= 128 ? 2 : 1) void k_cache_attent
             if (!side) {
                 const float2 other = ml[tid];
                 top = fmaxf(m, other.x);
-                const float f = m == -INFINITY && l == 0.0f ? 0.0f : exp2f(m - top);  // a NaN among the scores stays one
-                const float g = other.x == -INFINITY && other.y == 0.0f ? 0.0f : exp2f(other.x - top);
+                const float f = exp2f(m - top), g = exp2f(other.x - top);
                 m = top;
                 l = l * f + other.y * g;
 #pragma unroll
@@ -841,14 +817,13 @@ __global__ __launch_bounds__(256) void k_cache_attention_join_shares(CacheAttent
     if (row >= min(s.n, a.seq.max_new) * group) return;
     const float2 *const ml = (const float2 *)(a.partial + a.part_rows * D);
     float4v x = {};
-    float top = -INFINITY, sum = 0.0f;
+    float top = kNothing, sum = 0.0f;
     for (int k = share - 1;;) {
         const int64_t part = (2 * (int64_t)k + (k < share)) * kTileRows + at;
         const float2 p = ml[part];
         const float4v y = *(const float4v *)(a.partial + part * D + 4 * c);
         const float up = fmaxf(top, p.x);
-        const float f = top == -INFINITY && sum == 0.0f ? 0.0f : exp2f(top - up);  // a NaN among the scores stays one
-        const float g = p.x == -INFINITY && p.y == 0.0f ? 0.0f : exp2f(p.x - up);
+        const float f = exp2f(top - up), g = exp2f(p.x - up);
         top = up;
         sum = sum * f + p.y * g;
         x = x * f + y * g;
@@ -905,8 +880,8 @@ __global__ __launch_bounds__(256) void k_cache_attention_join(CacheAttentionArgs
     const float2 *const ml = (const float2 *)(a.partial + a.part_rows * D);
     const float *const o = a.partial + 4 * c;
     float4v x = {};
-    float top = -INFINITY, sum = 0.0f;
-    auto factor = [&](float2 p) { return p.x == -INFINITY && p.y == 0.0f ? 0.0f : exp2f(p.x - top); };  // a NaN among the scores stays one
+    float top = kNothing, sum = 0.0f;
+    auto factor = [&](float2 p) { return exp2f(p.x - top); };
     if constexpr (ALONE) {
         float2 p[kFewSplits];
         float4v y[kFewSplits];
@@ -919,7 +894,7 @@ __global__ __launch_bounds__(256) void k_cache_attention_join(CacheAttentionArgs
         if (t >= s.n) return;
 #pragma unroll
         for (int k = 0; k < kFewSplits; ++k) {
-            if (k >= parts) p[k] = make_float2(-INFINITY, 0.0f), y[k] = float4v{};
+            if (k >= parts) p[k] = make_float2(kNothing, 0.0f), y[k] = float4v{};
             top = fmaxf(top, p[k].x);
         }
 #pragma unroll
@@ -933,7 +908,7 @@ __global__ __launch_bounds__(256) void k_cache_attention_join(CacheAttentionArgs
         float2 p[kMostParts / 256];
         float4v early[kEarly];
 #pragma unroll
-        for (int j = 0; j < kMostParts / 256; ++j) p[j] = tid + 256 * j < parts ? ml[at(tid + 256 * j)] : make_float2(-INFINITY, 0.0f);
+        for (int j = 0; j < kMostParts / 256; ++j) p[j] = tid + 256 * j < parts ? ml[at(tid + 256 * j)] : make_float2(kNothing, 0.0f);
 #pragma unroll
         for (int j = 0; j < kEarly; ++j) early[j] = nth + j * kSide < parts ? *(const float4v *)(o + at(nth + j * kSide) * D) : float4v{};
         if (t >= s.n) return;

@@ -77,3 +77,59 @@ def test_values_at_the_end_of_the_range_stay_finite(lens, new, heads, kv, dim, m
     for c, v in enumerate((65504.0, -65504.0, 65504.0, -65504.0)):
         assert (out[:, :, c] == v).all()
     assert (out[:, :, 4:].abs() < 65504).all()
+
+
+def held(g, n, kv, dim, dtype, nats, big):
+    """n tokens of which the 100th rules: its score is `nats` above the others', its value 0 but for the last channel, where it is `big`.
+    -> reference cache and table"""
+    K, V = torch.randn((n, kv, dim), generator=g) * 0.5, 1.0 + 0.5 * torch.randn((n, kv, dim), generator=g)
+    K[:, :, 0], K[100, :, 0], K[100, :, 1] = 0.0, nats, 0.0
+    V[100], V[100, :, dim - 1] = 0.0, big
+    blocks = -(-n // 64)
+    table = torch.randperm(blocks, generator=g).to(torch.int32)[None]
+    ref = R.Cache(blocks, kv, 64, dim)
+    ref.write(K.to(dtype).double().numpy(), V.to(dtype).double().numpy(), table, [n], [0, n], 1)
+    return ref, table
+
+
+def bounded(k, v, size, q, alpha, dtype):
+    """(out, its bound, lse, its bound) of one query over all of a head's n keys and values, size[j] the scale of v[j].  A weight times
+    scale is rounded to 2^-11 of itself or 2^-36 of the row's largest; scores are off by ds as everywhere; fp32 sums of 16 keys
+    at a time, n / 16 of them, by 2^-24 each; then one rounding."""
+    n = len(k)
+    s = alpha * (k @ q)
+    w = np.exp(s - s.max())
+    W = w.sum()
+    out = w @ v / W
+    ds = float((alpha * (np.abs(k) @ np.abs(q))).max()) * 2.0 ** -16 + 2.0 ** -20
+    each = 2.0 ** -11 + 2 * ds + n / 16 * 2.0 ** -24
+    small = 2.0 ** -36 * (w * size).max() * (np.abs(v) / size[:, None]).sum(0) / W
+    eps = torch.finfo(dtype).eps / 2
+    return out, 1.01 * ((w @ np.abs(v)) / W * each + small) + eps * np.abs(out) + eps * float(torch.finfo(dtype).smallest_normal), s.max() + np.log(W), ds + 2.0 ** -19 + n / 16 * 2.0 ** -24
+
+
+@pytest.mark.parametrize("dtype,nats,big", [(f16, 15.0, 0.0), (f16, 18.0, 64.0), (b16, 26.0, 0.0), (b16, 15.0, 4096.0)])
+@pytest.mark.parametrize("n,batch,new,heads,kv,dim,how", [
+    (20000, 1, 1, 2, 1, 128, "parts"), (20000, 64, 1, 8, 8, 64, "shares"), (16000, 32, 3, 16, 2, 64, "parts"), (20000, 1, 40, 2, 1, 64, "parts"),
+    (16000, 1, 8400, 2, 2, 128, "whole"), (16000, 1, 8400, 8, 4, 64, "whole"), (131072, 1, 17000, 2, 1, 64, "shares"), (30000, 2, 4200, 2, 1, 256, "whole")])
+def test_the_tail_behind_a_key_that_rules(n, batch, new, heads, kv, dim, how, dtype, nats, big):
+    """A result that many small weights make, next to one that is 2^22 to 2^38 times as large: rows whose keys one wavefront goes over
+    alone, and in parts and shares."""
+    assert layout(batch * new, heads, kv, dim, batch, new, n) == how
+    g = torch.Generator().manual_seed(51)
+    ref, table = held(g, n, kv, dim, dtype, nats, big)
+    some = torch.zeros((8, dim), dtype=dtype)  # eight queries, all rows and heads have one of them
+    some[:, 0], some[:, 1] = 1.0, torch.randn(8, generator=g).to(dtype)
+    rows = torch.arange(batch * new) % 8
+    Q = some[rows][:, None].expand(-1, heads, -1).contiguous()
+    out, lse, _ = run(ref, ref.device(B), Q, table.expand(batch, -1).contiguous(), [n] * batch, [new] * batch, heads, 1.0, False, 0, max_len=n)
+    K, V, _ = ref.rows(table, 0, n)
+    group = heads // kv
+    for h in range(kv):
+        for i in range(min(8, batch * new)):
+            size = np.repeat(2.0 ** ref.ve[table[0].numpy(), h].astype(float), 64)[:n]
+            want, tol, log, tol_log = bounded(K[:, h], V[:, h], size, some[i].double().numpy(), 1.0, dtype)
+            mine = (rows == i).to(DEV)
+            err = np.abs(out[mine][:, h * group:(h + 1) * group].double().cpu().numpy() - want)
+            assert (err <= tol).all(), (h, i, (err / tol).max())
+            assert (np.abs(lse[mine][:, h * group:(h + 1) * group].double().cpu().numpy() - log) <= tol_log).all()
