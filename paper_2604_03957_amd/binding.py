@@ -457,6 +457,26 @@ def _dense(dtype, *xs):
                 raise ValueError("a tensor of strides %s has to be contiguous" % (tuple(x.stride()),))
 
 
+def _apart(x, given, width):
+    """How far apart the rows of an operator on heads are: as given, or as they are in the tensor, whose last dimensions, `width` elements
+    or more together, are a row ([M, width or more], [M, heads, dim], [batch, tokens, heads, dim]) and lie side by side."""
+    if isinstance(x, torch.Tensor) and x.numel() and width > 0:
+        size, i = 1, x.dim()
+        while i > 0 and size < width:
+            i -= 1
+            if x.shape[i] > 1 and x.stride(i) != size:
+                raise ValueError("a row's heads lie side by side, got shape %s and strides %s for rows of %d" % (tuple(x.shape), tuple(x.stride()), width))
+            size *= x.shape[i]
+        if given is None:
+            apart = None  # of the rows in the dimensions so far, and how far the next dimension's have to be
+            for n, stride in reversed([d for d in zip(x.shape[:i], x.stride()) if d[0] > 1]):
+                if apart is not None and stride != step:
+                    raise ValueError("rows are not equally far apart, got shape %s and strides %s: pass ld" % (tuple(x.shape), tuple(x.stride())))
+                apart, step = stride if apart is None else apart, stride * n
+            return width if apart is None else apart
+    return width if given is None else given
+
+
 def _here(*xs):
     """These calls launch on the current device: tensors have to be there."""
     for x in xs:
@@ -496,29 +516,31 @@ def bwta_head_norm_rope(Q, K, wq, wk, positions, inv_freq, Qout, Kout, *, M, hea
     _here(Q, K, wq, wk, positions, inv_freq, Qout, Kout)
     _dense(torch.int32, positions)
     _dense(torch.float32, inv_freq)
-    ldq = heads * dim if ldq is None else ldq
-    ldk = kv_heads * dim if ldk is None else ldk
-    _check(_lib.bwta_head_norm_rope(_ptr(Q), ldq, heads, _ptr(wq), _ptr(K), ldk, kv_heads, _ptr(wk),
-                                    _dtype(dtype, *((K, wk, Kout) if Q is None else (Q, K, wq, wk, Qout, Kout))),
+    dtype = _dtype(dtype, *((K, wk, Kout) if Q is None else (Q, K, wq, wk, Qout, Kout)))
+    wide, kv_wide = heads * dim, kv_heads * dim
+    _check(_lib.bwta_head_norm_rope(_ptr(Q), _apart(Q, ldq, wide), heads, _ptr(wq), _ptr(K), _apart(K, ldk, kv_wide), kv_heads, _ptr(wk), dtype,
                                     M, dim, int(norm), eps, _ptr(positions), _ptr(inv_freq), dim if rot_dim is None else rot_dim, int(interleaved),
-                                    _ptr(Qout), heads * dim if ldqo is None else ldqo, _ptr(Kout), kv_heads * dim if ldko is None else ldko,
-                                    _stream(stream)))
+                                    _ptr(Qout), _apart(Qout, ldqo, wide), _ptr(Kout), _apart(Kout, ldko, kv_wide), _stream(stream)))
 
 
-def _ldt(table, given):
+def _ldt(table, given, batch):
     if isinstance(table, torch.Tensor) and (table.dtype != torch.int32 or (table.dim() and table.stride(-1) != 1 and table.shape[-1] > 1)):
         raise TypeError("a block table is int32, its rows without gaps, got %s of strides %s" % (table.dtype, tuple(table.stride())))
     if given is not None:
         return given
-    return 0 if table is None or isinstance(table, int) else table.stride(0)
+    if table is None or isinstance(table, int) or table.dim() == 0:
+        return 0
+    if batch == 1 and (table.dim() == 1 or table.shape[0] == 1):
+        return table.numel()  # one row, whatever its stride
+    return table.stride(0)
 
 
 def _cache_rows(call, cache, K, V, table, lens, cu, M, batch, max_new, max_len, ldk, ldv, ldt, dtype, stream):
     _here(cache, K, V, table, lens, cu)
     _dense(torch.int32, lens, cu)
-    width = cache.kv_heads * cache.dim
-    _check(call(cache, _ptr(K), width if ldk is None else ldk, _ptr(V), width if ldv is None else ldv, _dtype(dtype, K, V), _ptr(table),
-                _ldt(table, ldt), _ptr(lens), _ptr(cu), batch, M, max_new, max_len, _stream(stream)))
+    width, dtype = cache.kv_heads * cache.dim, _dtype(dtype, K, V)
+    _check(call(cache, _ptr(K), _apart(K, ldk, width), _ptr(V), _apart(V, ldv, width), dtype, _ptr(table), _ldt(table, ldt, batch), _ptr(lens), _ptr(cu), batch, M,
+                max_new, max_len, _stream(stream)))
 
 
 def bwta_cache_write(cache, K, V, table, lens, cu=None, *, M, batch, max_new, max_len, ldk=None, ldv=None, ldt=None, dtype=None, stream=None):
@@ -538,10 +560,10 @@ def bwta_cache_attention(cache, Q, out, lse, table, lens, cu=None, workspace=Non
     _here(cache, Q, out, lse, table, lens, cu, workspace)
     _dense(torch.int32, lens, cu)
     _dense(torch.float32, lse)
-    width = heads * cache.dim
-    _check(_lib.bwta_cache_attention(cache, _ptr(Q), width if ldq is None else ldq, _ptr(out), width if ldo is None else ldo, _dtype(dtype, Q, out),
-                                     _ptr(lse), _ptr(table), _ldt(table, ldt), _ptr(lens), _ptr(cu), batch, M, max_new, max_len, heads, alpha,
-                                     int(causal), window, _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream)))
+    width, dtype = heads * cache.dim, _dtype(dtype, Q, out)
+    _check(_lib.bwta_cache_attention(cache, _ptr(Q), _apart(Q, ldq, width), _ptr(out), _apart(out, ldo, width), dtype, _ptr(lse), _ptr(table),
+                                     _ldt(table, ldt, batch), _ptr(lens), _ptr(cu), batch, M, max_new, max_len, heads, alpha, int(causal), window, _ptr(workspace),
+                                     _nbytes(workspace, workspace_bytes), _stream(stream)))
 
 
 def _native_identity():

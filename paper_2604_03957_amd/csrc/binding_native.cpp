@@ -138,11 +138,11 @@ struct Here {
         if (t && t->dim() && t->stride(-1) != 1 && t->size(-1) > 1) throw NotOrdinary{};
         return t;
     }
-    void *rows_like(PyObject *o, const at::Tensor *first) const
+    const at::Tensor *rows_like(PyObject *o, const at::Tensor *first) const
     {
         const at::Tensor *t = rows(o);
         if (t && first && t->scalar_type() != first->scalar_type()) throw NotOrdinary{};
-        return ::address(t);
+        return t;
     }
     void *dense(PyObject *o, at::ScalarType type) const
     {
@@ -204,7 +204,37 @@ int flag(PyObject *o, bool otherwise)
     return o == Py_True;
 }
 
-int64_t rows_apart(PyObject *o, int64_t width) { return given(o) ? int64(o) : width; }
+// binding._apart
+int64_t rows_apart(PyObject *o, const at::Tensor *t, int64_t width)
+{
+    if (t && t->numel() && width > 0) {
+        int64_t size = 1, i = t->dim();
+        while (i > 0 && size < width) {
+            --i;
+            if (t->size(i) > 1 && t->stride(i) != size) throw NotOrdinary{};
+            size *= t->size(i);
+        }
+        if (!given(o)) {
+            int64_t apart = 0, step = 0;
+            while (i-- > 0) {
+                if (t->size(i) <= 1) continue;
+                if (step && t->stride(i) != step) throw NotOrdinary{};
+                if (!step) apart = t->stride(i);
+                step = t->stride(i) * t->size(i);
+                if (step == 0) throw NotOrdinary{};
+            }
+            return step ? apart : width;
+        }
+    }
+    return given(o) ? int64(o) : width;
+}
+
+int64_t blocks_apart(PyObject *o, const at::Tensor *table, int batch)
+{
+    if (given(o)) return int64(o);
+    if (!table || table->dim() == 0) throw NotOrdinary{};
+    return batch == 1 && (table->dim() == 1 || table->size(0) == 1) ? table->numel() : table->stride(0);
+}
 
 // the C call without the interpreter lock (a launch waits where the queue is full), its code turned into what the Python
 // form returns or raises
@@ -392,15 +422,15 @@ bool head_norm_rope(const Bound &b, PyObject *const *v, PyObject **result)
 {
     const Here h = here(v[21]);
     const at::Tensor *Q = h.rows(v[0]), *K = h.rows(v[1]), *first = Q ? Q : K;
-    const int M = int32(v[8]), heads = int32(v[9]), kv = int32(v[10]), dim = int32(v[11]), rot = (int)rows_apart(v[12], dim);
-    if (given(v[12])) int32(v[12]);
+    h.rows_like(v[1], first);
+    const at::Tensor *wqt = h.rows_like(v[2], first), *wkt = h.rows_like(v[3], first), *Qout = h.rows_like(v[6], first), *Kout = h.rows_like(v[7], first);
+    const int M = int32(v[8]), heads = int32(v[9]), kv = int32(v[10]), dim = int32(v[11]), rot = given(v[12]) ? int32(v[12]) : dim;
     const float eps = number(v[13], 1e-6f);
     const int norm = flag(v[14], true), interleaved = flag(v[15], false);
     const int64_t wq = (int64_t)heads * dim, wk = (int64_t)kv * dim;
-    const int64_t ldq = rows_apart(v[16], wq), ldk = rows_apart(v[17], wk), ldqo = rows_apart(v[18], wq), ldko = rows_apart(v[19], wk);
+    const int64_t ldq = rows_apart(v[16], Q, wq), ldk = rows_apart(v[17], K, wk), ldqo = rows_apart(v[18], Qout, wq), ldko = rows_apart(v[19], Kout, wk);
     const int dtype = head_dtype(v[20], first);
-    void *const pq = address(Q), *const pk = h.rows_like(v[1], first), *const pwq = h.rows_like(v[2], first), *const pwk = h.rows_like(v[3], first),
-               *const qo = h.rows_like(v[6], first), *const ko = h.rows_like(v[7], first);
+    void *const pq = address(Q), *const pk = address(K), *const pwq = address(wqt), *const pwk = address(wkt), *const qo = address(Qout), *const ko = address(Kout);
     const int32_t *const pos = h.ints(v[4]);
     const float *const freq = h.floats(v[5]);
     BWTA_FN(bwta_head_norm_rope);
@@ -412,13 +442,12 @@ bool cache_rows(F *call, PyObject *const *v, PyObject **result)
 {
     const Here h = here(v[14]);
     const Cache cache = cache_of(v[0], h);
-    const at::Tensor *K = h.rows(v[1]), *table = h.table(v[3]);
+    const at::Tensor *K = h.rows(v[1]), *V = h.rows_like(v[2], K), *table = h.table(v[3]);
     const int M = int32(v[6]), batch = int32(v[7]), max_new = int32(v[8]), max_len = int32(v[9]);
-    const int64_t width = (int64_t)cache.c.kv_heads * cache.c.dim, ldk = rows_apart(v[10], width), ldv = rows_apart(v[11], width);
-    if (!given(v[12]) && (!table || table->dim() == 0)) throw NotOrdinary{};
-    const int64_t ldt = rows_apart(v[12], table ? table->stride(0) : 0);
+    const int64_t width = (int64_t)cache.c.kv_heads * cache.c.dim, ldk = rows_apart(v[10], K, width), ldv = rows_apart(v[11], V, width);
+    const int64_t ldt = blocks_apart(v[12], table, batch);
     const int dtype = head_dtype(v[13], K);
-    void *const pk = address(K), *const pv = h.rows_like(v[2], K), *const pt = address(table);
+    void *const pk = address(K), *const pv = address(V), *const pt = address(table);
     const int32_t *const lens = h.ints(v[4]), *const cu = h.ints(v[5]);
     return finish([&] { return call(&cache.c, pk, ldk, pv, ldv, dtype, (const int32_t *)pt, ldt, lens, cu, batch, M, max_new, max_len, h.stream); }, result);
 }
@@ -439,17 +468,16 @@ bool cache_attention(const Bound &b, PyObject *const *v, PyObject **result)
 {
     const Here h = here(v[21]);
     const Cache cache = cache_of(v[0], h);
-    const at::Tensor *Q = h.rows(v[1]), *table = h.table(v[4]), *ws = h.tensor(v[7]);
+    const at::Tensor *Q = h.rows(v[1]), *out = h.rows_like(v[2], Q), *table = h.table(v[4]), *ws = h.tensor(v[7]);
     const int M = int32(v[8]), batch = int32(v[9]), max_new = int32(v[10]), max_len = int32(v[11]), heads = int32(v[12]);
     if (!v[13]) throw NotOrdinary{};
     const float alpha = number(v[13], 0.0f);
     const int causal = flag(v[14], true), window = v[15] ? int32(v[15]) : 0;
-    const int64_t width = (int64_t)heads * cache.c.dim, ldq = rows_apart(v[16], width), ldo = rows_apart(v[17], width);
-    if (!given(v[18]) && (!table || table->dim() == 0)) throw NotOrdinary{};
-    const int64_t ldt = rows_apart(v[18], table ? table->stride(0) : 0);
+    const int64_t width = (int64_t)heads * cache.c.dim, ldq = rows_apart(v[16], Q, width), ldo = rows_apart(v[17], out, width);
+    const int64_t ldt = blocks_apart(v[18], table, batch);
     const int dtype = head_dtype(v[19], Q);
     const size_t bytes = bytes_of(v[20], ws);
-    void *const pq = address(Q), *const po = h.rows_like(v[2], Q), *const pt = address(table), *const pws = address(ws);
+    void *const pq = address(Q), *const po = address(out), *const pt = address(table), *const pws = address(ws);
     float *const lse = h.floats(v[3]);
     const int32_t *const lens = h.ints(v[5]), *const cu = h.ints(v[6]);
     BWTA_FN(bwta_cache_attention);

@@ -1,0 +1,40 @@
+"""Where the Python forms of the operators on heads look for the rows of a tensor (no GPU needed)."""
+import pytest
+import torch
+
+from paper_2604_03957_amd import binding as B
+
+
+def test_rows_are_as_far_apart_as_the_tensors():
+    wide = torch.zeros((5, 12, 64), dtype=torch.float16)  # a fused projection: 4 + 4 + 4 heads of 64
+    width = 4 * 64
+    for x in (wide[:, :4], wide[:, 4:8], wide, wide.view(5, -1), wide.view(5, -1)[:, 64:], wide[:, :4].unsqueeze(1), wide.view(5, 1, -1)):
+        assert B._apart(x, None, width) == 12 * 64
+    assert B._apart(wide[::2, :4], None, width) == 24 * 64
+    assert B._apart(torch.zeros((2, 5, 12, 64))[:, :, :4], None, width) == 12 * 64  # [batch, tokens, heads, dim]
+    dense = torch.zeros((5, 4, 64))
+    for x in (dense, dense.view(5, -1), dense.view(-1), dense.view(20, 64), dense[:1], wide[:1, :4], dense.view(5, 2, 2, 64), dense[:0], None, 1 << 20, torch.zeros((2, 5, 256))):
+        assert B._apart(x, None, width) == width
+    assert B._apart(torch.zeros((5, 1, 64)), None, 64) == 64 and B._apart(torch.zeros((5, 3, 64))[:, :1], None, 64) == 192
+    assert B._apart(wide, 999, width) == 999 and B._apart(None, 999, width) == 999 and B._apart(wide, None, 0) == 0
+
+
+def test_rows_that_are_none_are_refused():
+    wide = torch.zeros((5, 12, 64), dtype=torch.float16)
+    for x in (wide[:, ::2], wide.transpose(0, 1), wide[:, :4].transpose(1, 2), wide[:, 0]):  # every second head, heads first, elements apart, one head of rows of four
+        for ld in (None, 12 * 64):
+            with pytest.raises(ValueError):
+                B._apart(x, ld, 4 * 64)
+    uneven = torch.zeros((2, 7, 4, 64))[:, :5]
+    with pytest.raises(ValueError):
+        B._apart(uneven, None, 4 * 64)
+    assert B._apart(uneven, 256, 4 * 64) == 256
+
+
+def test_a_table_of_one_row():
+    t = torch.zeros((7, 1), dtype=torch.int32)
+    assert B._ldt(t.T, None, 1) == 7 and B._ldt(t.view(-1), None, 1) == 7 and B._ldt(t.view(1, 7), None, 1) == 7
+    assert B._ldt(torch.zeros((3, 9), dtype=torch.int32)[:, :7], None, 3) == 9 and B._ldt(t, None, 7) == 1 and B._ldt(t, 5, 1) == 5
+    assert B._ldt(None, None, 1) == 0 and B._ldt(4096, 6, 1) == 6
+    with pytest.raises(TypeError):
+        B._ldt(t.long(), None, 1)
