@@ -477,6 +477,17 @@ def _apart(x, given, width):
     return width if given is None else given
 
 
+def _span(x):
+    """Bytes from a tensor's first element to behind its last."""
+    return (1 + sum((n - 1) * stride for n, stride in zip(x.shape, x.stride()))) * x.element_size() if x.numel() else 0
+
+
+def _holds(x, apart, rows, width, size):
+    """A tensor has the `rows` rows of `width` elements of `size` bytes that a call reads or writes of it."""
+    if isinstance(x, torch.Tensor) and rows > 0 and width > 0 and _span(x) < ((rows - 1) * apart + width) * size:
+        raise ValueError("%d rows of %d, %d apart, are not in a tensor of shape %s and strides %s" % (rows, width, apart, tuple(x.shape), tuple(x.stride())))
+
+
 def _here(*xs):
     """These calls launch on the current device: tensors have to be there."""
     for x in xs:
@@ -517,10 +528,17 @@ def bwta_head_norm_rope(Q, K, wq, wk, positions, inv_freq, Qout, Kout, *, M, hea
     _dense(torch.int32, positions)
     _dense(torch.float32, inv_freq)
     dtype = _dtype(dtype, *((K, wk, Kout) if Q is None else (Q, K, wq, wk, Qout, Kout)))
-    wide, kv_wide = heads * dim, kv_heads * dim
-    _check(_lib.bwta_head_norm_rope(_ptr(Q), _apart(Q, ldq, wide), heads, _ptr(wq), _ptr(K), _apart(K, ldk, kv_wide), kv_heads, _ptr(wk), dtype,
-                                    M, dim, int(norm), eps, _ptr(positions), _ptr(inv_freq), dim if rot_dim is None else rot_dim, int(interleaved),
-                                    _ptr(Qout), _apart(Qout, ldqo, wide), _ptr(Kout), _apart(Kout, ldko, kv_wide), _stream(stream)))
+    wide, kv_wide, rot_dim = heads * dim, kv_heads * dim, dim if rot_dim is None else rot_dim
+    ldq, ldk, ldqo, ldko = _apart(Q, ldq, wide), _apart(K, ldk, kv_wide), _apart(Qout, ldqo, wide), _apart(Kout, ldko, kv_wide)
+    for x, ld, w in ((Q, ldq, wide), (K, ldk, kv_wide), (Qout, ldqo, wide), (Kout, ldko, kv_wide)):
+        _holds(x, ld, M, w, 2)
+    if M > 0:
+        _holds(wq, 0, int(norm and heads > 0), dim, 2)
+        _holds(wk, 0, int(norm and kv_heads > 0), dim, 2)
+        _holds(positions, 0, int(rot_dim > 0), M, 4)
+        _holds(inv_freq, 0, 1, rot_dim // 2, 4)
+    _check(_lib.bwta_head_norm_rope(_ptr(Q), ldq, heads, _ptr(wq), _ptr(K), ldk, kv_heads, _ptr(wk), dtype, M, dim, int(norm), eps, _ptr(positions),
+                                    _ptr(inv_freq), rot_dim, int(interleaved), _ptr(Qout), ldqo, _ptr(Kout), ldko, _stream(stream)))
 
 
 def _ldt(table, given, batch):
@@ -535,12 +553,22 @@ def _ldt(table, given, batch):
     return table.stride(0)
 
 
+def _sequences_hold(cache, table, ldt, lens, cu, M, batch, max_new, max_len):
+    if M > 0 and batch > 0 and max_new > 0:
+        _holds(lens, 0, 1, batch, 4)
+        _holds(cu, 0, 1, batch + 1, 4)
+        _holds(table, ldt, batch, -(-max_len // cache.block) if cache.block > 0 else 0, 4)
+
+
 def _cache_rows(call, cache, K, V, table, lens, cu, M, batch, max_new, max_len, ldk, ldv, ldt, dtype, stream):
     _here(cache, K, V, table, lens, cu)
     _dense(torch.int32, lens, cu)
     width, dtype = cache.kv_heads * cache.dim, _dtype(dtype, K, V)
-    _check(call(cache, _ptr(K), _apart(K, ldk, width), _ptr(V), _apart(V, ldv, width), dtype, _ptr(table), _ldt(table, ldt, batch), _ptr(lens), _ptr(cu), batch, M,
-                max_new, max_len, _stream(stream)))
+    ldk, ldv, ldt = _apart(K, ldk, width), _apart(V, ldv, width), _ldt(table, ldt, batch)
+    _holds(K, ldk, M, width, 2)
+    _holds(V, ldv, M, width, 2)
+    _sequences_hold(cache, table, ldt, lens, cu, M, batch, max_new, max_len)
+    _check(call(cache, _ptr(K), ldk, _ptr(V), ldv, dtype, _ptr(table), ldt, _ptr(lens), _ptr(cu), batch, M, max_new, max_len, _stream(stream)))
 
 
 def bwta_cache_write(cache, K, V, table, lens, cu=None, *, M, batch, max_new, max_len, ldk=None, ldv=None, ldt=None, dtype=None, stream=None):
@@ -561,9 +589,13 @@ def bwta_cache_attention(cache, Q, out, lse, table, lens, cu=None, workspace=Non
     _dense(torch.int32, lens, cu)
     _dense(torch.float32, lse)
     width, dtype = heads * cache.dim, _dtype(dtype, Q, out)
-    _check(_lib.bwta_cache_attention(cache, _ptr(Q), _apart(Q, ldq, width), _ptr(out), _apart(out, ldo, width), dtype, _ptr(lse), _ptr(table),
-                                     _ldt(table, ldt, batch), _ptr(lens), _ptr(cu), batch, M, max_new, max_len, heads, alpha, int(causal), window, _ptr(workspace),
-                                     _nbytes(workspace, workspace_bytes), _stream(stream)))
+    ldq, ldo, ldt = _apart(Q, ldq, width), _apart(out, ldo, width), _ldt(table, ldt, batch)
+    _holds(Q, ldq, M, width, 2)
+    _holds(out, ldo, M, width, 2)
+    _holds(lse, heads, M, heads, 4)
+    _sequences_hold(cache, table, ldt, lens, cu, M, batch, max_new, max_len)
+    _check(_lib.bwta_cache_attention(cache, _ptr(Q), ldq, _ptr(out), ldo, dtype, _ptr(lse), _ptr(table), ldt, _ptr(lens), _ptr(cu), batch, M, max_new, max_len, heads,
+                                     alpha, int(causal), window, _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream)))
 
 
 def _native_identity():

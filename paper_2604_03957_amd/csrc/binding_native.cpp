@@ -144,14 +144,14 @@ struct Here {
         if (t && first && t->scalar_type() != first->scalar_type()) throw NotOrdinary{};
         return t;
     }
-    void *dense(PyObject *o, at::ScalarType type) const
+    const at::Tensor *dense(PyObject *o, at::ScalarType type) const
     {
         const at::Tensor *t = tensor(o);
         if (t && (t->scalar_type() != type || !t->is_contiguous())) throw NotOrdinary{};
-        return ::address(t);
+        return t;
     }
-    int32_t *ints(PyObject *o) const { return (int32_t *)dense(o, at::kInt); }
-    float *floats(PyObject *o) const { return (float *)dense(o, at::kFloat); }
+    const at::Tensor *ints(PyObject *o) const { return dense(o, at::kInt); }
+    const at::Tensor *floats(PyObject *o) const { return dense(o, at::kFloat); }
     const at::Tensor *table(PyObject *o) const
     {
         const at::Tensor *t = rows(o);
@@ -227,6 +227,24 @@ int64_t rows_apart(PyObject *o, const at::Tensor *t, int64_t width)
         }
     }
     return given(o) ? int64(o) : width;
+}
+
+// binding._holds (in 128 bits: what does not fit 64 is the Python form's to refuse)
+void holds(const at::Tensor *t, int64_t apart, int64_t rows, int64_t width, int64_t size)
+{
+    if (!t || rows <= 0 || width <= 0) return;
+    __int128 span = t->numel() ? 1 : 0;
+    if (span)
+        for (int64_t i = 0; i < t->dim(); ++i) span += (__int128)(t->size(i) - 1) * t->stride(i);
+    if (span * (int64_t)t->element_size() < ((__int128)(rows - 1) * apart + width) * size) throw NotOrdinary{};
+}
+
+void sequences_hold(const Cache &cache, const at::Tensor *table, int64_t ldt, const at::Tensor *lens, const at::Tensor *cu, int M, int batch, int max_new, int max_len)
+{
+    if (M <= 0 || batch <= 0 || max_new <= 0) return;
+    holds(lens, 0, 1, batch, 4);
+    holds(cu, 0, 1, (int64_t)batch + 1, 4);
+    if (cache.c.block > 0) holds(table, ldt, batch, ((int64_t)max_len + cache.c.block - 1) / cache.c.block, 4);
 }
 
 int64_t blocks_apart(PyObject *o, const at::Tensor *table, int batch)
@@ -431,8 +449,14 @@ bool head_norm_rope(const Bound &b, PyObject *const *v, PyObject **result)
     const int64_t ldq = rows_apart(v[16], Q, wq), ldk = rows_apart(v[17], K, wk), ldqo = rows_apart(v[18], Qout, wq), ldko = rows_apart(v[19], Kout, wk);
     const int dtype = head_dtype(v[20], first);
     void *const pq = address(Q), *const pk = address(K), *const pwq = address(wqt), *const pwk = address(wkt), *const qo = address(Qout), *const ko = address(Kout);
-    const int32_t *const pos = h.ints(v[4]);
-    const float *const freq = h.floats(v[5]);
+    const at::Tensor *const positions = h.ints(v[4]), *const inv_freq = h.floats(v[5]);
+    holds(Q, ldq, M, wq, 2), holds(K, ldk, M, wk, 2), holds(Qout, ldqo, M, wq, 2), holds(Kout, ldko, M, wk, 2);
+    if (M > 0) {
+        holds(wqt, 0, norm && heads > 0, dim, 2), holds(wkt, 0, norm && kv > 0, dim, 2);
+        holds(positions, 0, rot > 0, M, 4), holds(inv_freq, 0, 1, rot / 2, 4);
+    }
+    const int32_t *const pos = (const int32_t *)address(positions);
+    const float *const freq = (const float *)address(inv_freq);
     BWTA_FN(bwta_head_norm_rope);
     return finish([&] { return call(pq, ldq, heads, pwq, pk, ldk, kv, pwk, dtype, M, dim, norm, eps, pos, freq, rot, interleaved, qo, ldqo, ko, ldko, h.stream); }, result);
 }
@@ -447,8 +471,11 @@ bool cache_rows(F *call, PyObject *const *v, PyObject **result)
     const int64_t width = (int64_t)cache.c.kv_heads * cache.c.dim, ldk = rows_apart(v[10], K, width), ldv = rows_apart(v[11], V, width);
     const int64_t ldt = blocks_apart(v[12], table, batch);
     const int dtype = head_dtype(v[13], K);
+    const at::Tensor *const lt = h.ints(v[4]), *const ct = h.ints(v[5]);
+    holds(K, ldk, M, width, 2), holds(V, ldv, M, width, 2);
+    sequences_hold(cache, table, ldt, lt, ct, M, batch, max_new, max_len);
     void *const pk = address(K), *const pv = address(V), *const pt = address(table);
-    const int32_t *const lens = h.ints(v[4]), *const cu = h.ints(v[5]);
+    const int32_t *const lens = (const int32_t *)address(lt), *const cu = (const int32_t *)address(ct);
     return finish([&] { return call(&cache.c, pk, ldk, pv, ldv, dtype, (const int32_t *)pt, ldt, lens, cu, batch, M, max_new, max_len, h.stream); }, result);
 }
 
@@ -478,8 +505,11 @@ bool cache_attention(const Bound &b, PyObject *const *v, PyObject **result)
     const int dtype = head_dtype(v[19], Q);
     const size_t bytes = bytes_of(v[20], ws);
     void *const pq = address(Q), *const po = address(out), *const pt = address(table), *const pws = address(ws);
-    float *const lse = h.floats(v[3]);
-    const int32_t *const lens = h.ints(v[5]), *const cu = h.ints(v[6]);
+    const at::Tensor *const logs = h.floats(v[3]), *const lt = h.ints(v[5]), *const ct = h.ints(v[6]);
+    holds(Q, ldq, M, width, 2), holds(out, ldo, M, width, 2), holds(logs, heads, M, heads, 4);
+    sequences_hold(cache, table, ldt, lt, ct, M, batch, max_new, max_len);
+    float *const lse = (float *)address(logs);
+    const int32_t *const lens = (const int32_t *)address(lt), *const cu = (const int32_t *)address(ct);
     BWTA_FN(bwta_cache_attention);
     return finish([&] { return call(&cache.c, pq, ldq, po, ldo, dtype, lse, (const int32_t *)pt, ldt, lens, cu, batch, M, max_new, max_len,
                                     heads, alpha, causal, window, pws, bytes, h.stream); }, result);

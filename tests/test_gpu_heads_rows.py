@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from paper_2604_03957_amd import binding as B
+from test_gpu_heads_binding import _calls
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -84,3 +85,20 @@ def test_a_table_of_one_row_of_any_stride():
             torch.cuda.synchronize()
             got.append(out)
     assert all(torch.equal(x, got[0]) for x in got) and got[0].abs().max() > 0
+
+
+def test_short_tensors_are_refused_before_anything_is_launched():
+    """Whoever marshals: one row, entry or length where the call's sizes say more."""
+    for name, make, kw, written in _calls(torch.float16):
+        for i, x in enumerate(make()):
+            if not isinstance(x, torch.Tensor) or (name == "bwta_cache_attention" and i == 7):
+                continue
+            for how in (0, 2):
+                a = make()
+                whole = a[i]
+                a[i] = whole[:1]
+                before = [a[j].clone() for j in written if isinstance(a[j], torch.Tensor)] + [whole.clone()]
+                with pytest.raises(ValueError):
+                    forms(name)[how](*a, **kw)
+                torch.cuda.synchronize()
+                assert all(torch.equal(b, y) for b, y in zip(before, [a[j] for j in written if isinstance(a[j], torch.Tensor)] + [whole]))

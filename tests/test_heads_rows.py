@@ -38,3 +38,28 @@ def test_a_table_of_one_row():
     assert B._ldt(None, None, 1) == 0 and B._ldt(4096, 6, 1) == 6
     with pytest.raises(TypeError):
         B._ldt(t.long(), None, 1)
+
+
+def test_short_tensors_are_refused():
+    """What a call would read or write behind a tensor's last element."""
+    x = torch.zeros((5, 4, 64), dtype=torch.float16)
+    for t, apart, rows, width in ((x, 256, 5, 256), (x, 256, 0, 256), (x, 256, -1, 256), (x, 512, 3, 256), (x[:, :2], 256, 5, 128), (x[1:], 256, 4, 256), (x[:0], 256, 5, 0),
+                                  (None, 256, 9, 256), (4096, 256, 9, 256)):
+        B._holds(t, apart, rows, width, 2)
+    for t, apart, rows, width in ((x, 256, 6, 256), (x, 264, 5, 256), (x, 256, 5, 257), (x[:, :2], 256, 5, 129), (x[:, 1:], 256, 5, 256), (x[:0], 256, 1, 256), (x[1:], 256, 5, 256),
+                                  (x.view(torch.uint8)[:, :, :64], 256, 5, 256)):
+        with pytest.raises(ValueError):
+            B._holds(t, apart, rows, width, 2)
+
+
+def test_short_lengths_offsets_and_tables_are_refused():
+    cache = B.Cache(4096, 4096, 4096, 4096, 8, 2, 64, 128)
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    good = dict(table=i32(3, 4), ldt=4, lens=i32(3), cu=i32(4), M=9, batch=3, max_new=3, max_len=250)
+    B._sequences_hold(cache, **good)
+    B._sequences_hold(cache, **dict(good, table=i32(3, 7)[:, 2:6], ldt=7, cu=None))
+    for empty in (dict(M=0), dict(batch=0), dict(max_new=0)):
+        B._sequences_hold(cache, **dict(good, lens=i32(0), **empty))
+    for bad in (dict(lens=i32(2)), dict(cu=i32(3)), dict(table=i32(2, 4)), dict(max_len=257), dict(table=i32(3, 3)), dict(table=i32(3, 7)[:, 4:], ldt=7)):
+        with pytest.raises(ValueError):
+            B._sequences_hold(cache, **dict(good, **bad))
