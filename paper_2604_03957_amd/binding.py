@@ -436,6 +436,11 @@ def _dtype(dtype, x, *others):
         if isinstance(y, torch.Tensor) and y.dim() and y.stride(-1) != 1 and y.shape[-1] > 1:
             raise ValueError("elements of a row lie next to each other, got strides %s" % (tuple(y.stride()),))
     if dtype is not None:
+        if dtype in (DTYPE_FP16, DTYPE_BF16):
+            named = torch.float16 if dtype == DTYPE_FP16 else torch.bfloat16
+            for y in (x, *others):  # of that type, or the bits of it as whole numbers
+                if isinstance(y, torch.Tensor) and y.dtype not in (named, torch.int16, torch.uint16):
+                    raise TypeError("dtype= says %s, a tensor is %s" % (named, y.dtype))
         return dtype
     try:
         given = {torch.float16: DTYPE_FP16, torch.bfloat16: DTYPE_BF16}[x.dtype]

@@ -190,11 +190,14 @@ Cache cache_of(PyObject *o, const Here &h)
     return c;
 }
 
-int head_dtype(PyObject *o, const at::Tensor *t)
+int head_dtype(PyObject *o, const at::Tensor *t)  // (that the others are of the first tensor's type is rows_like's to see)
 {
-    if (given(o)) return int32(o);
-    if (!t || (t->scalar_type() != at::kHalf && t->scalar_type() != at::kBFloat16)) throw NotOrdinary{};
-    return t->scalar_type() == at::kHalf ? BWTA_DTYPE_FP16 : BWTA_DTYPE_BF16;
+    if (t && t->scalar_type() != at::kHalf && t->scalar_type() != at::kBFloat16) throw NotOrdinary{};
+    const int named = given(o) ? int32(o) : -1;
+    if (!t) return given(o) ? named : throw NotOrdinary{};
+    const int mine = t->scalar_type() == at::kHalf ? BWTA_DTYPE_FP16 : BWTA_DTYPE_BF16;
+    if ((named == BWTA_DTYPE_FP16 || named == BWTA_DTYPE_BF16) && named != mine) throw NotOrdinary{};
+    return given(o) ? named : mine;
 }
 
 int flag(PyObject *o, bool otherwise)

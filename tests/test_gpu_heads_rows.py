@@ -102,3 +102,17 @@ def test_short_tensors_are_refused_before_anything_is_launched():
                     forms(name)[how](*a, **kw)
                 torch.cuda.synchronize()
                 assert all(torch.equal(b, y) for b, y in zip(before, [a[j] for j in written if isinstance(a[j], torch.Tensor)] + [whole]))
+
+
+def test_a_given_type_that_is_not_the_tensors_is_refused():
+    for name, make, kw, written in _calls(torch.float16):
+        for how in (0, 2):
+            a = make()
+            before = [a[j].clone() for j in written if isinstance(a[j], torch.Tensor)]
+            with pytest.raises(TypeError):
+                forms(name)[how](*a, **dict(kw, dtype=B.DTYPE_BF16))
+            torch.cuda.synchronize()
+            assert all(torch.equal(b, a[j]) for b, j in zip(before, [j for j in written if isinstance(a[j], torch.Tensor)]))
+        for call in forms(name):
+            assert call(*make(), **dict(kw, dtype=B.DTYPE_FP16)) is None
+    torch.cuda.synchronize()

@@ -63,3 +63,13 @@ def test_short_lengths_offsets_and_tables_are_refused():
     for bad in (dict(lens=i32(2)), dict(cu=i32(3)), dict(table=i32(2, 4)), dict(max_len=257), dict(table=i32(3, 3)), dict(table=i32(3, 7)[:, 4:], ldt=7)):
         with pytest.raises(ValueError):
             B._sequences_hold(cache, **dict(good, **bad))
+
+
+def test_a_given_type_is_the_tensors():
+    half, brain, bits = torch.zeros(4, dtype=torch.float16), torch.zeros(4, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int16)
+    for dtype, xs in ((B.DTYPE_FP16, (half, half)), (B.DTYPE_BF16, (brain, None)), (B.DTYPE_FP16, (bits, 4096)), (B.DTYPE_BF16, (bits, brain)), (B.DTYPE_FP16, (None, 4096)),
+                      (B.DTYPE_INT8, (half, brain)), (9, (half,))):  # the last two are the library's to refuse
+        assert B._dtype(dtype, *xs) == dtype
+    for dtype, xs in ((B.DTYPE_FP16, (brain,)), (B.DTYPE_BF16, (half,)), (B.DTYPE_FP16, (half, brain)), (B.DTYPE_FP16, (half.float(),)), (B.DTYPE_BF16, (None, brain.view(torch.uint8)))):
+        with pytest.raises(TypeError):
+            B._dtype(dtype, *xs)
