@@ -556,6 +556,14 @@ static bool rows_clash(const void *a, int64_t lda, int a_heads, const void *out,
     return rows_overlap(a, lda, a_heads * dim, out, ldo, o_heads * dim, M);
 }
 
+// a result's M rows of `width` elements against `bytes` that lie in a row (which may lie between those rows)
+static bool rows_hit(const void *out, int64_t ldo, int64_t width, int M, const void *p, int64_t bytes)
+{
+    const int64_t from = (int64_t)((uintptr_t)p - (uintptr_t)out), ld = 2 * ldo, row = from < 0 ? 0 : from / ld;
+    if (!p || bytes <= 0 || from + bytes <= 0 || row >= M) return false;
+    return from < 0 || from - row * ld < 2 * width || (row + 1 < M && (row + 1) * ld < from + bytes);
+}
+
 int bwta_head_norm_rope(const void *Q, int64_t ldq, int heads, const void *wq, const void *K, int64_t ldk, int kv_heads,
                         const void *wk, int dtype, int M, int dim, int norm, float eps, const int32_t *positions,
                         const float *inv_freq, int rot_dim, int interleaved, void *Qout, int64_t ldqo, void *Kout,
@@ -578,6 +586,11 @@ int bwta_head_norm_rope(const void *Q, int64_t ldq, int heads, const void *wq, c
     if (heads && kv_heads && (rows_clash(Q, ldq, heads, Kout, ldko, kv_heads, M, dim, false) || rows_clash(K, ldk, kv_heads, Qout, ldqo, heads, M, dim, false) ||
                               rows_clash(Qout, ldqo, heads, Kout, ldko, kv_heads, M, dim, false)))
         return BWTA_ERR_UNSUPPORTED;
+    auto written = [&](const void *p, int64_t bytes) {
+        return (heads && rows_hit(Qout, ldqo, (int64_t)heads * dim, M, p, bytes)) || (kv_heads && rows_hit(Kout, ldko, (int64_t)kv_heads * dim, M, p, bytes));
+    };
+    if ((norm && heads && written(wq, 2 * dim)) || (norm && kv_heads && written(wk, 2 * dim))) return BWTA_ERR_UNSUPPORTED;
+    if (rot_dim && (written(positions, 4 * (int64_t)M) || written(inv_freq, 2 * rot_dim))) return BWTA_ERR_UNSUPPORTED;
     const bwta::HeadRopeArgs a{{Q, K}, {Qout, Kout}, {norm ? wq : nullptr, norm ? wk : nullptr}, {ldq, ldk}, {ldqo, ldko}, {heads, kv_heads},
                                M, dim, rot_dim, norm != 0, interleaved != 0, dtype == BWTA_DTYPE_BF16, eps, positions, inv_freq};
     return hip_result(bwta::launch_head_norm_rope(a, (hipStream_t)stream));
