@@ -558,6 +558,14 @@ def _ldt(table, given, batch):
     return table.stride(0)
 
 
+def _room(workspace, given):
+    """Bytes of a workspace: a contiguous tensor's own, or as many of them as are given."""
+    n = _nbytes(workspace, given)
+    if isinstance(workspace, torch.Tensor) and (not workspace.is_contiguous() or n > workspace.nbytes):
+        raise ValueError("a workspace of %d bytes is not in a tensor of shape %s and strides %s" % (n, tuple(workspace.shape), tuple(workspace.stride())))
+    return n
+
+
 def _sequences_hold(cache, table, ldt, lens, cu, M, batch, max_new, max_len):
     if M > 0 and batch > 0 and max_new > 0:
         _holds(lens, 0, 1, batch, 4)
@@ -600,7 +608,7 @@ def bwta_cache_attention(cache, Q, out, lse, table, lens, cu=None, workspace=Non
     _holds(lse, heads, M, heads, 4)
     _sequences_hold(cache, table, ldt, lens, cu, M, batch, max_new, max_len)
     _check(_lib.bwta_cache_attention(cache, _ptr(Q), ldq, _ptr(out), ldo, dtype, _ptr(lse), _ptr(table), ldt, _ptr(lens), _ptr(cu), batch, M, max_new, max_len, heads,
-                                     alpha, int(causal), window, _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream)))
+                                     alpha, int(causal), window, _ptr(workspace), _room(workspace, workspace_bytes), _stream(stream)))
 
 
 def _native_identity():

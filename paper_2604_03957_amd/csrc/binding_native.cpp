@@ -507,6 +507,7 @@ bool cache_attention(const Bound &b, PyObject *const *v, PyObject **result)
     const int64_t ldt = blocks_apart(v[18], table, batch);
     const int dtype = head_dtype(v[19], Q);
     const size_t bytes = bytes_of(v[20], ws);
+    if (ws && (!ws->is_contiguous() || bytes > ws->nbytes())) throw NotOrdinary{};  // binding._room
     void *const pq = address(Q), *const po = address(out), *const pt = address(table), *const pws = address(ws);
     const at::Tensor *const logs = h.floats(v[3]), *const lt = h.ints(v[5]), *const ct = h.ints(v[6]);
     holds(Q, ldq, M, width, 2), holds(out, ldo, M, width, 2), holds(logs, heads, M, heads, 4);

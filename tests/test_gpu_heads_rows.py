@@ -116,3 +116,15 @@ def test_a_given_type_that_is_not_the_tensors_is_refused():
         for call in forms(name):
             assert call(*make(), **dict(kw, dtype=B.DTYPE_FP16)) is None
     torch.cuda.synchronize()
+
+
+def test_a_workspace_that_is_not_there_is_refused():
+    name, make, kw, _ = [c for c in _calls(torch.float16) if c[0] == "bwta_cache_attention" and len(c[1]()) == 8][0]
+    for how in (0, 2):
+        for ws, more in ((torch.zeros(1, dtype=torch.uint8, device=DEV).expand(1 << 20), {}), (torch.zeros(4096, dtype=torch.uint8, device=DEV), dict(workspace_bytes=1 << 20))):
+            a = make()
+            a[7] = ws
+            with pytest.raises(ValueError):
+                forms(name)[how](*a, **kw, **more)
+            torch.cuda.synchronize()
+            assert (a[2] == 3).all() and (ws == 0).all()

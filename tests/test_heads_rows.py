@@ -73,3 +73,11 @@ def test_a_given_type_is_the_tensors():
     for dtype, xs in ((B.DTYPE_FP16, (brain,)), (B.DTYPE_BF16, (half,)), (B.DTYPE_FP16, (half, brain)), (B.DTYPE_FP16, (half.float(),)), (B.DTYPE_BF16, (None, brain.view(torch.uint8)))):
         with pytest.raises(TypeError):
             B._dtype(dtype, *xs)
+
+
+def test_a_workspace_is_in_its_tensor():
+    ws = torch.zeros(512, dtype=torch.uint8)
+    assert B._room(ws, None) == 512 and B._room(ws, 256) == 256 and B._room(None, None) == 0 and B._room(4096, 1 << 30) == 1 << 30 and B._room(ws.view(torch.float32)[64:], None) == 256
+    for x, n in ((ws, 513), (ws[::2], None), (ws[:1].expand(1 << 20), None), (ws[:1].expand(1 << 20), 1)):
+        with pytest.raises(ValueError):
+            B._room(x, n)
