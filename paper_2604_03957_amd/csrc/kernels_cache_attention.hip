@@ -955,9 +955,12 @@ void launch(const CacheAttentionArgs &a, const AttentionPlan &plan, hipStream_t 
     constexpr int NB = D < 256 ? 2 : 1, kTwice = D < 256 ? 2 * kAttWaves : kAttWaves;
     const dim3 grid((unsigned)plan.groups), block(kAttWaves * 64);
     if (plan.rows > 32) {
-        // Two workgroups' worth of wavefronts on the same rows halve the way of the rows that see most, which is what few
-        // workgroups take their time for; many balance by themselves.  us, one / two, heads of 128: a causal prompt of 2048 with 32
-        // heads 58 / 55, two of them 95 / 109; 128 rows over 256 keys, 32 times, 40 / 56.
+        // Two workgroups' worth of wavefronts on the same rows halve the way of the rows that see most.  That gains where a round
+        // holds all (a compute unit has one such workgroup at a time, or two of the others), and in whole prompts, whose ends
+        // see most and are few.  us, one / two, heads of 64 and of 128: 256 tiles of 2048 keys 37 / 33 and 54 / 52, 320 of them
+        // 50 / 58 and 73 / 91; a prompt of 2048, 24 heads 36 / 30 and 52 / 45, 32 heads 37 / 36 and 56 / 55; of 1536, 40
+        // heads 29 / 30 and 44 / 46; of 1024, 64 heads 22 / 25 and 34 / 38; 2048 with a window of 1024, 32 heads 30 / 36 and 46 / 56;
+        // 2048 rows behind 2048 keys, 32 heads 83 / 82 and 127 / 130; 384 tiles of 328 keys of 64 15.6 / 20.9.
         constexpr int kMost = D <= 128 ? 2 : 1;
         if constexpr (D <= 128) {
             if (a.share_log2 >= 0) {
@@ -966,7 +969,8 @@ void launch(const CacheAttentionArgs &a, const AttentionPlan &plan, hipStream_t 
                 return;
             }
         }
-        if (kMost == 2 && plan.reach >= 1024 && plan.groups <= 512)
+        const bool prompt = a.causal && !a.window && plan.reach < 2 * (int64_t)a.seq.max_new;
+        if (kMost == 2 && plan.reach >= 1024 && (plan.groups <= 256 || (prompt && plan.groups <= 512 && plan.reach >= 4 * plan.groups)))
             hipLaunchKernelGGL((k_cache_attention_rows<T, D, kMost, false>), grid, dim3(kMost * 256), 0, st, a, plan.row_tiles);
         else
             hipLaunchKernelGGL((k_cache_attention_rows<T, D, 1, false>), grid, block, 0, st, a, plan.row_tiles);
