@@ -58,8 +58,19 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417
 
 constexpr float kHighest = 15.0f, kPlace = 11.0f;  // exponents of weights: where m has to move, and what the moved one leaves
 constexpr float kNothing = -3e38f;                  // m before any key has been seen
-// m for keys of which the largest has exponent e.  (As it was for a NaN, and for the -Inf of keys that are not seen.)
-__device__ __forceinline__ float moved(float e, float m) { return e > m + kHighest ? e - kPlace : m; }
+// m for keys of which the largest has exponent e.  (As it was for a NaN, and for the -Inf of keys that are not seen.)  On a grid of
+// 2^-16, so that what is added to it below, whole numbers, is exact; that largest one's weight is 2^kPlace but for 2^-17 of it.
+__device__ __forceinline__ float moved(float e, float m)
+{
+    if (!(e > m + kHighest)) return m;
+    const float x = e - kPlace;
+    return fabsf(x) < 128.0f ? rintf(x * 65536.0f) * (1.0f / 65536.0f) : x;
+}
+// The natural logarithm of l 2^m, rounded once: m and l's exponent join first.
+__device__ __forceinline__ float log_of(float m, float l)
+{
+    return fmaf(m + (float)__builtin_amdgcn_frexp_expf(l), kLn2, kLn2 * log2f(__builtin_amdgcn_frexp_mantf(l)));
+}
 
 // The larger one; a NaN if either is one (which saves making a quiet one of it first).
 __device__ __forceinline__ float most(float x, float y) { return __builtin_elementwise_maximum(x, y); }
@@ -118,7 +129,7 @@ __device__ __forceinline__ void give(const CacheAttentionArgs &a, const Seq &s, 
     const int64_t token = s.row + t;
     const float f = l == 0.0f ? 0.0f : 1.0f / l;
     *(uint2 *)((T *)a.out + token * a.ldo + (int64_t)h * D + channel) = result<T>(x, f);
-    if (once && a.lse) a.lse[token * a.heads + h] = kLn2 * (m + log2f(l));
+    if (once && a.lse) a.lse[token * a.heads + h] = log_of(m, l);
 }
 
 // Workgroups that share `total` steps, as a power of two: not more than there are, so that everybody has one; and where the
@@ -944,7 +955,7 @@ __global__ __launch_bounds__(256) void k_cache_attention_join(CacheAttentionArgs
     const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
     const int64_t token = s.row + t;
     *(uint2 *)((T *)a.out + token * a.ldo + (int64_t)h * D + 4 * c) = result<T>(x, f);
-    if (c == 0 && a.lse) a.lse[token * a.heads + h] = kLn2 * (top + log2f(sum));
+    if (c == 0 && a.lse) a.lse[token * a.heads + h] = log_of(top, sum);
 }
 
 constexpr int kAttWaves = 4;

@@ -133,3 +133,31 @@ def test_the_tail_behind_a_key_that_rules(n, batch, new, heads, kv, dim, how, dt
             err = np.abs(out[mine][:, h * group:(h + 1) * group].double().cpu().numpy() - want)
             assert (err <= tol).all(), (h, i, (err / tol).max())
             assert (np.abs(lse[mine][:, h * group:(h + 1) * group].double().cpu().numpy() - log) <= tol_log).all()
+
+
+@pytest.mark.parametrize("size", [2.0 ** -40, 2.0 ** -12, 1.0, 2.0 ** 30])
+@pytest.mark.parametrize("batch,new,heads,kv,dim,max_len,how", [(60, 1, 2, 1, 64, 700, "whole"), (20, 1, 4, 2, 128, 3000, "parts"), (300, 1, 4, 2, 64, 20000, "shares"), (140, 140, 1, 1, 64, 700, "whole"),
+                                                                (140, 140, 1, 1, 256, 700, "whole"), (3, 70, 2, 1, 128, 5000, "parts"), (52, 70, 6, 3, 64, 5000, "shares")])
+def test_log_sums_of_exact_scores_are_rounded_once(batch, new, heads, kv, dim, max_len, how, size):
+    """Scores that are whole numbers of bits, so weights and their sums are exact: the logarithm is off by its own rounding, 2^-24 of it,
+    and by that of a fraction's logarithm and of ln 2, less than 2^-22 together, whatever the values' scale is."""
+    alpha = np.float32(1) / np.float32(1.44269504088896340736)
+    assert np.float32(alpha * np.float32(1.44269504088896340736)) == 1
+    assert layout(batch * new, heads, kv, dim, batch, new, max_len) == how
+    g = torch.Generator().manual_seed(71)
+    n = 700
+    blocks = -(-n // 64)
+    K, V = torch.zeros((n, kv, dim)), torch.randn((n, kv, dim), generator=g) * size
+    K[:, :, 0] = -torch.randint(0, 13, (n, kv), generator=g).float()
+    table = torch.randperm(blocks, generator=g).to(torch.int32)[None]
+    ref = R.Cache(blocks, kv, 64, dim)
+    ref.write(K.double().numpy(), V.bfloat16().double().numpy(), table, [n], [0, n], 1)
+    lens = [int(torch.randint(1, n + 1, (1,), generator=g)) for _ in range(batch)]
+    Q = torch.zeros((batch * new, heads, dim), dtype=b16)
+    Q[:, :, 0] = 1.0
+    wide = torch.cat([table, torch.full((1, -(-max_len // 64) - blocks), -1, dtype=torch.int32)], dim=1) if max_len > n else table
+    lse = run(ref, ref.device(B), Q, wide.expand(batch, -1).contiguous(), lens, [new] * batch, heads, float(alpha), False, 0, max_len=max_len)[1].double().cpu().numpy()
+    sums = np.cumsum(2.0 ** K[:, :, 0].double().numpy(), axis=0)  # exact
+    want = np.log(sums[np.array(lens) - 1])[:, None, :, None]  # the same for a sequence's rows and a key head's queries
+    got = lse.reshape(batch, new, kv, heads // kv)
+    assert (np.abs(got - want) <= 2.0 ** -23 * np.abs(want) + 2.0 ** -22).all(), np.abs(got - want).max()
