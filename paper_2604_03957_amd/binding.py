@@ -493,6 +493,20 @@ def _holds(x, apart, rows, width, size):
         raise ValueError("%d rows of %d, %d apart, are not in a tensor of shape %s and strides %s" % (rows, width, apart, tuple(x.shape), tuple(x.stride())))
 
 
+def _rows(x, given, M, width):
+    """_apart, and _holds for M such rows of 16-bit elements: the forms that most calls have at once, others by those two."""
+    if not isinstance(x, torch.Tensor):
+        return width if given is None else given
+    shape, strides = x.shape, x.stride()
+    if M > 0 and width > 0 and len(shape) in (2, 3) and strides[-1] == 1 and shape[0] >= M and x.element_size() == 2:
+        size = shape[1] if len(shape) == 2 else shape[1] * shape[2] if strides[1] == shape[2] < width else 0
+        if size >= width and (given is None or M == 1 or given == strides[0]):
+            return given if given is not None else strides[0] if shape[0] > 1 else width
+    apart = _apart(x, given, width)
+    _holds(x, apart, M, width, 2)
+    return apart
+
+
 def _here(*xs):
     """These calls launch on the current device: tensors have to be there."""
     for x in xs:
@@ -534,14 +548,9 @@ def bwta_head_norm_rope(Q, K, wq, wk, positions, inv_freq, Qout, Kout, *, M, hea
     _dense(torch.float32, inv_freq)
     dtype = _dtype(dtype, *((K, wk, Kout) if Q is None else (Q, K, wq, wk, Qout, Kout)))
     wide, kv_wide, rot_dim = heads * dim, kv_heads * dim, dim if rot_dim is None else rot_dim
-    ldq, ldk, ldqo, ldko = _apart(Q, ldq, wide), _apart(K, ldk, kv_wide), _apart(Qout, ldqo, wide), _apart(Kout, ldko, kv_wide)
-    for x, ld, w in ((Q, ldq, wide), (K, ldk, kv_wide), (Qout, ldqo, wide), (Kout, ldko, kv_wide)):
-        _holds(x, ld, M, w, 2)
+    ldq, ldk, ldqo, ldko = _rows(Q, ldq, M, wide), _rows(K, ldk, M, kv_wide), _rows(Qout, ldqo, M, wide), _rows(Kout, ldko, M, kv_wide)
     if M > 0:
-        _holds(wq, 0, int(norm and heads > 0), dim, 2)
-        _holds(wk, 0, int(norm and kv_heads > 0), dim, 2)
-        _holds(positions, 0, int(rot_dim > 0), M, 4)
-        _holds(inv_freq, 0, 1, rot_dim // 2, 4)
+        _counts((wq, dim if norm and heads > 0 else 0), (wk, dim if norm and kv_heads > 0 else 0), (positions, M if rot_dim > 0 else 0), (inv_freq, rot_dim // 2))
     _check(_lib.bwta_head_norm_rope(_ptr(Q), ldq, heads, _ptr(wq), _ptr(K), ldk, kv_heads, _ptr(wk), dtype, M, dim, int(norm), eps, _ptr(positions),
                                     _ptr(inv_freq), rot_dim, int(interleaved), _ptr(Qout), ldqo, _ptr(Kout), ldko, _stream(stream)))
 
@@ -566,20 +575,26 @@ def _room(workspace, given):
     return n
 
 
+def _counts(*xs):
+    """Tensors without gaps have as many elements as a call reads of them."""
+    for x, n in xs:
+        if isinstance(x, torch.Tensor) and x.numel() < n:
+            raise ValueError("a tensor of %d elements, the call's sizes say %d" % (x.numel(), n))
+
+
 def _sequences_hold(cache, table, ldt, lens, cu, M, batch, max_new, max_len):
     if M > 0 and batch > 0 and max_new > 0:
-        _holds(lens, 0, 1, batch, 4)
-        _holds(cu, 0, 1, batch + 1, 4)
-        _holds(table, ldt, batch, -(-max_len // cache.block) if cache.block > 0 else 0, 4)
+        _counts((lens, batch), (cu, batch + 1))
+        blocks = -(-max_len // cache.block) if cache.block > 0 else 0
+        if not (isinstance(table, torch.Tensor) and table.dim() == 2 and table.shape[0] >= batch and table.shape[1] >= blocks and table.stride(0) == ldt):
+            _holds(table, ldt, batch, blocks, 4)
 
 
 def _cache_rows(call, cache, K, V, table, lens, cu, M, batch, max_new, max_len, ldk, ldv, ldt, dtype, stream):
     _here(cache, K, V, table, lens, cu)
     _dense(torch.int32, lens, cu)
     width, dtype = cache.kv_heads * cache.dim, _dtype(dtype, K, V)
-    ldk, ldv, ldt = _apart(K, ldk, width), _apart(V, ldv, width), _ldt(table, ldt, batch)
-    _holds(K, ldk, M, width, 2)
-    _holds(V, ldv, M, width, 2)
+    ldk, ldv, ldt = _rows(K, ldk, M, width), _rows(V, ldv, M, width), _ldt(table, ldt, batch)
     _sequences_hold(cache, table, ldt, lens, cu, M, batch, max_new, max_len)
     _check(call(cache, _ptr(K), ldk, _ptr(V), ldv, dtype, _ptr(table), ldt, _ptr(lens), _ptr(cu), batch, M, max_new, max_len, _stream(stream)))
 
@@ -602,10 +617,8 @@ def bwta_cache_attention(cache, Q, out, lse, table, lens, cu=None, workspace=Non
     _dense(torch.int32, lens, cu)
     _dense(torch.float32, lse)
     width, dtype = heads * cache.dim, _dtype(dtype, Q, out)
-    ldq, ldo, ldt = _apart(Q, ldq, width), _apart(out, ldo, width), _ldt(table, ldt, batch)
-    _holds(Q, ldq, M, width, 2)
-    _holds(out, ldo, M, width, 2)
-    _holds(lse, heads, M, heads, 4)
+    ldq, ldo, ldt = _rows(Q, ldq, M, width), _rows(out, ldo, M, width), _ldt(table, ldt, batch)
+    _counts((lse, M * heads if M > 0 and heads > 0 else 0))
     _sequences_hold(cache, table, ldt, lens, cu, M, batch, max_new, max_len)
     _check(_lib.bwta_cache_attention(cache, _ptr(Q), ldq, _ptr(out), ldo, dtype, _ptr(lse), _ptr(table), ldt, _ptr(lens), _ptr(cu), batch, M, max_new, max_len, heads,
                                      alpha, int(causal), window, _ptr(workspace), _room(workspace, workspace_bytes), _stream(stream)))

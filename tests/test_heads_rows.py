@@ -81,3 +81,25 @@ def test_a_workspace_is_in_its_tensor():
     for x, n in ((ws, 513), (ws[::2], None), (ws[:1].expand(1 << 20), None), (ws[:1].expand(1 << 20), 1)):
         with pytest.raises(ValueError):
             B._room(x, n)
+
+
+def test_the_quick_form_of_the_checks_is_the_same_checks():
+    half = lambda *s: torch.zeros(s, dtype=torch.float16)  # noqa: E731
+    wide = half(5, 12, 64)
+    tensors = [wide, wide[:, :4], wide[:, 4:8], wide[:, ::2], wide.view(5, -1), wide.view(5, -1)[:, 64:], wide[:1], wide[:1, :4], wide[::2, :4], half(5, 4, 64), half(20, 64), half(1280), half(2, 5, 4, 64),
+               half(5, 1, 256), half(5, 300), half(0, 256), wide[:, :4].transpose(0, 1), half(1, 256).expand(5, 256), half(5, 4, 64).float(), None, 4096]
+    for x in tensors:
+        for M in (-1, 0, 1, 2, 5, 6):
+            for width in (0, 64, 256, 320):
+                for given in (None, 256, 300, 768):
+                    def both():
+                        apart = B._apart(x, given, width)
+                        B._holds(x, apart, M, width, 2)
+                        return apart
+                    results = []
+                    for f in (both, lambda: B._rows(x, given, M, width)):
+                        try:
+                            results.append(f())
+                        except ValueError:
+                            results.append("refused")
+                    assert results[0] == results[1], (x if x is None or isinstance(x, int) else (x.shape, x.stride()), M, width, given)
