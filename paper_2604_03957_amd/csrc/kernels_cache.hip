@@ -6,8 +6,8 @@
 // each takes from memory is then 16 bytes in a row.
 //
 // Bound by memory: a block's tokens are read once and its codes written once.  Prompts of 2019 to 4001 tokens of 8 heads of
-// 128 in and back out (207 MB) take 41 us, 5.0 TB/s; whole contexts back to bf16 (236 MB) 40 to 46 us, 5.1 to 5.9 TB/s, where a
-// copy reaches 4.9; a decode step's 64 tokens 4.8 us, the latency of table, tokens and scale one after the other.
+// 128 in and back out (207 MB) take 41 us, 5.0 TB/s; whole contexts back to bf16 (236 MB) 39 to 51 us from one run and machine to
+// another, 4.6 to 6.0 TB/s, where a copy reaches 4.9; a decode step's 64 tokens 4.8 us, the latency of table, tokens and scale one after the other.
 #include "bwta_heads.h"
 
 namespace bwta {

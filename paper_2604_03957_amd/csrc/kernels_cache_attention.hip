@@ -144,7 +144,9 @@ __device__ __forceinline__ int *shares_of(const CacheAttentionArgs &a) { return 
 // needs in registers and nothing in LDS until their sums are joined; 16 rows is what the matrix cores take anyway, so heads that
 // share their keys cost nothing.  Bound by the cache's bytes: 64 sequences of 2048 to 8192 tokens, 32 heads on 8 of 128 (680 MB)
 // take 119 us, 5.7 TB/s, equal ones of 8192 6.4 TB/s; one token over 131072 keys (268 MB) 48.8 us with the join, over 2048 keys
-// of 32 heads (17 MB) 9.7 us, most of it the latency of lengths, table and codes one after the other, and of a second launch.
+// of 32 heads (17 MB) 9.5 us, most of it the latency of lengths, table and codes one after the other, and of a second launch.
+// 17 to 32 rows of heads of 128 take all the registers of a SIMD for one wavefront, or in workgroups of eight, which need two on
+// a SIMD, leave some in scratch, which they read outside the steps.
 template <typename T, int D, int NB, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, (NB == 1 && D <= 128) ? 2 : 1) void k_cache_attention(CacheAttentionArgs a)
 {
@@ -440,11 +442,14 @@ __device__ __forceinline__ int4 *begins_of(const CacheAttentionArgs &a) { return
 // With SHARES workgroups share all steps equally: those of a sequence's first head's first 128 rows, second 128 and so on, next
 // head, next sequence.  What begins or ends inside somebody else's share becomes a part, and each leaves where it begins for
 // the join.
-// Bound by issue: a step of 32 rows is 1024 cycles of matrix cores beside some 1000 of vector ALU (32 weights a lane with a
-// fused multiply-add, a power, an addition and half a conversion each, and the widening), and 32 KB from LDS a wavefront.
-// 8192 keys for each of 2048 rows, 32 heads of 128: 920 TFLOP/s with two groups and 970 with one, where a large fp16 product
+// A step of 32 rows of heads of 128 is 1024 cycles of matrix cores and some 1100 of vector ALU (32 weights a lane with a fused
+// multiply-add, a power, an addition and half a conversion each, and the widening), and 32 KB from LDS a wavefront.  Counted in
+// chunks of long prompts, a SIMD takes 2400 cycles a step: matrix cores are busy 43 % of them, the vector ALU 50 %, seldom both.
+// Its two wavefronts wait for their turn to issue 28 % of their time, and 26 % for memory, LDS and each other.  8192 keys for each
+// of 2048 rows, 32 heads of 128: 980 TFLOP/s with one group, and 800 with two (16 heads, 1024 rows), where a large fp16 product
 // reaches 1322; 64 rows a wavefront need more registers than the vector ALU can address and copy sums between the two files at
-// every step (half as fast), codes widened by each wavefront cost it 128 conversions a step for 32 (5 % slower).
+// every step (half as fast), codes widened by each wavefront cost it 128 conversions a step for 32 (5 % slower).  Heads of 128
+// need 7 to 13 registers more than there are: 32 to 56 bytes a lane lie in scratch and are read at a tile's ends, outside the steps.
 template <typename T, int D, int GROUPS, bool SHARES>
 __global__ __launch_bounds__(GROUPS * 256, D <= 128 ? 2 : 1) void k_cache_attention_rows(CacheAttentionArgs a, int row_tiles)
 {
@@ -1060,9 +1065,9 @@ AttentionPlan cache_attention_plan(int heads, int kv_heads, int dim, int batch, 
     // Few rounds of workgroups, each with many steps: the last round is often half empty, and sequences differ.  Two workgroups
     // for every compute unit share all steps instead, unless rounds come out even or rows are so many that their ends differ
     // (a prompt's: tiles are taken longest first then, and those that run at a time read the same keys, which shares do not).
-    // us, tiles / shares, 32 heads on 8 of 128: 1200 rows and 4096 keys 119 / 102; 512 and 8192, three times, 267 / 241; up to 1024
-    // and 5163 to 16024, four times, 595 / 532.  Against that 512 and 32768 keys four times 1131 / 1154, 512 and 2048 four times
-    // 78 / 95, a prompt of 8192 572 / 615, 2048 and 32768 four times 4292 / 4950; heads of 256 lose registers.
+    // us, tiles / shares, 32 heads on 8 of 128: 1200 rows and 4096 keys 106 / 102; 512 and 8192, three times, 250 / 242 (heads of 64
+    // 170 / 153); up to 1024 and 5163 to 16024, four times, 652 / 548.  Against that 512 and 32768 keys four times 1119 / 1168,
+    // 512 and 2048 four times 74 / 96, a prompt of 8192 569 / 647, 2048 and 32768 four times 4314 / 4890; heads of 256 lose registers.
     const double all = p.groups * (double)steps, rounds = p.groups / 256, fill = rounds / (double)(int64_t)(rounds + 255.0 / 256);
     const bool few_rounds = p.groups > 256 && p.groups <= kMostShared, uneven = batch > 1 || fill < 0.85;
     if (dim < 256 && steps >= 64 && few_rounds && uneven && (int64_t)max_new * 2 <= reach && all < (double)(1u << 31)) {
@@ -1073,8 +1078,8 @@ AttentionPlan cache_attention_plan(int heads, int kv_heads, int dim, int batch, 
         return p;
     }
     // Parts of many rows are large: one round of workgroups at most, and four steps each at least.  (us, 100 rows and 2000 keys of
-    // 8 heads 15.9, with 16 steps 27.1; 33 rows of 8 heads on 2, 32768 keys 23.1 and 29.4; 88 rows of 36 heads and sequences, 6200
-    // keys, six parts each 31, eight, which are more than a round, 47.)
+    // 8 heads 15.9, with 16 steps 27.1; 33 rows of 8 heads on 2, 32768 keys 24.8 and 29.4; 88 rows of 36 heads and sequences, 6200
+    // keys, six parts each 29, eight, which are more than a round, 47.)
     const int64_t want = (int64_t)(256 / p.groups), most = steps / 4, s = want < most ? want : most;
     if (s <= 1) return p;
     p.splits = (int)s;

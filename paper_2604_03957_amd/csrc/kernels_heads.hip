@@ -3,8 +3,8 @@
 //   (y_a, y_b) -> (y_a cos t - y_b sin t, y_a sin t + y_b cos t),  t = position * inv_freq[pair]
 // and one rounding to 16 bits.  A pair is (i, i + rot/2), or (2i, 2i + 1) with `interleaved`; what is behind rot passes.
 //
-// Bound by memory: every element is read and written once.  8192 tokens of 32 + 8 heads of 128 in bf16 (168 MB) take 33.4 us,
-// 5.0 TB/s, what a copy of that size reaches; one token of 64 heads 3.3 us, a launch's latency.
+// Bound by memory: every element is read and written once.  8192 tokens of 32 + 8 heads of 128 in bf16 (168 MB) take 33.5 us,
+// 5.0 TB/s, what a copy of that size reaches; one token of 64 heads 3.2 us: a launch, position and frequencies, then the rows.
 #include "bwta_heads.h"
 
 namespace bwta {
