@@ -428,6 +428,9 @@ def bwta_gemm_grouped(problem_array, workspace, *, M, N, K, a_scale_mode=SCALE_V
 
 
 # ---- operators on heads ------------------------------------------------------------------------------
+#
+# Unless given, ld and ldt are as the tensors have their rows.  Tensors have to be on the current device, of the type that the
+# header or dtype= says, and hold what the call's sizes say; of addresses nothing of this is known.
 
 
 def _dtype(dtype, x, *others):
