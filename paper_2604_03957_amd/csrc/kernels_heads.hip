@@ -30,7 +30,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_head_norm_rope(HeadRopeArgs a, 
         for (int p = lane; p < half; p += 64) {
             const double turns = pos * (double)a.inv_freq[p] * 0.15915494309189533577, part = turns - rint(turns);
             const float r = 2.0f * (float)part, rest = (float)((part - 0.5 * (double)r) * 6.28318530717958647693);
-            const float c = cospif(r), s = sinpif(r);  // of the angle as fp32 has it; the rest, up to 1.9e-7, turns them the last bit
+            const float c = cospif(r), s = sinpif(r);  // of the angle as fp32 has it; the rest, up to 9.4e-8, turns them the last bit
             cs[wave][p] = make_float2(fmaf(-rest, s, c), fmaf(rest, c, s));
         }
     }
